@@ -288,6 +288,109 @@ mrem_status mrem_mix_inputs(mrem_ctx* ctx, const void* x_fp, const void* x_q, fl
                             void* hip_stream);
 
 /*
+ * Operators of a student's training pass outside the module step: rotary positions between projection and attention,
+ * attention with its gradients, and the loss on a teacher's top logits.  They need no context; errors are those of the
+ * calling thread (mrem_last_error(NULL)).  Work goes to the caller's stream only, nothing is allocated, and every call may
+ * be captured into a graph.  Sums, softmax statistics and angles are held in 32 bits or more; results are rounded once to
+ * `dtype` (mrem_dtype).  The same call on the same inputs gives the same bits.
+ *
+ * mrem_rotary_frequencies -- radians a position of each of the rotary_dim / 2 pairs, f_i = base^(-2i / rotary_dim), scaled for
+ * contexts `factor` times longer than the `trained` positions of training (host only):
+ *   MREM_ROTARY_PLAIN   as they are
+ *   MREM_ROTARY_LINEAR  f_i / factor
+ *   MREM_ROTARY_BASE    base * factor^(rotary_dim / (rotary_dim - 2)) in place of base (rotary_dim 2: as they are)
+ *   MREM_ROTARY_BANDS   k_i f_i + (1 - k_i) f_i / factor, where k_i rises linearly from 0 to 1 as the rotations trained * f_i / 2 pi
+ *                       of a pair rise from `slow` to `fast`
+ * rotary_dim even, >= 2; base, factor, trained > 0; fast > slow.  Those that a kind does not use are ignored.
+ */
+typedef enum { MREM_ROTARY_PLAIN = 0, MREM_ROTARY_LINEAR = 1, MREM_ROTARY_BASE = 2, MREM_ROTARY_BANDS = 3 } mrem_rotary_scaling;
+mrem_status mrem_rotary_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double trained, double fast,
+                                    double slow, double* freq /*host*/);
+/*
+ * mrem_rotary_forward -- turns the first rotary_dim values of each head by the angle a = position * freq[i] of each pair i,
+ *   y1 = amplitude (x1 cos a - x2 sin a),  y2 = amplitude (x2 cos a + x1 sin a),
+ * and copies the rest of the head.  Pair i is (i, i + rotary_dim / 2), or with interleaved = 1 (2 i, 2 i + 1).  Angles are formed
+ * in 64 bits.
+ * mrem_rotary_backward -- the gradient: the same with sin a -> -sin a (x: the gradient of y, y: the gradient of x).
+ *   x, y       device dtype [rows, heads, head_dim], heads contiguous, rows ld_x and ld_y elements apart; y may be x (ld_y = ld_x),
+ *              and may not overlap it otherwise
+ *   freq       device fp64 [rotary_dim / 2]
+ *   positions  device int32 [rows], any value, or NULL: row t is at position t % seq
+ * head_dim 1..512, rotary_dim even, 2..head_dim.  rows = 0 does nothing.  Pointers of x and y: 16-byte aligned.
+ */
+mrem_status mrem_rotary_forward(const void* x, void* y, int32_t dtype, int64_t rows, int32_t heads, int32_t head_dim, int64_t ld_x,
+                                int64_t ld_y, int32_t rotary_dim, int32_t interleaved, float amplitude, const double* freq,
+                                const int32_t* positions, int64_t seq, void* hip_stream);
+mrem_status mrem_rotary_backward(const void* dy, void* dx, int32_t dtype, int64_t rows, int32_t heads, int32_t head_dim, int64_t ld_dy,
+                                 int64_t ld_dx, int32_t rotary_dim, int32_t interleaved, float amplitude, const double* freq,
+                                 const int32_t* positions, int64_t seq, void* hip_stream);
+
+/*
+ * mrem_attention_forward, mrem_attention_backward -- softmax attention over sequences of any lengths, one behind the other or
+ * padded, with one key head for q_heads / kv_heads query heads each.
+ * Sequence b has the q_len[b] query rows from q_start[b] on and the k_len[b] key rows from k_start[b] on.  Its query i is at
+ * position p = i + k_len - q_len and sees the keys j < k_len, with causal = 1 only j <= p, and with window > 0 (causal only) of
+ * those only j > p - window.  For what it sees
+ *   s_j = scale q.k_j,  lse = log sum exp s_j,  out = sum exp(s_j - lse) v_j;   a query that sees nothing: out = 0, lse = -inf,
+ * and a gradient of zero.  The backward pass recomputes the probabilities from lse; gradients of a key head are sums over its
+ * query heads, in a fixed order.
+ *   q, out, d_out, dq   device dtype [q_rows, q_heads, head_dim], rows ld_q (q, dq) and ld_out (out, d_out) elements apart
+ *   k, dk; v, dv        device dtype [k_rows, kv_heads, head_dim], rows ld_k and ld_v elements apart (so the three of them, and
+ *                       their gradients, may lie side by side in one buffer)
+ *   q_start, k_start    device int32 [batch + 1], not falling, the last one the end of the last sequence; or NULL: b * rows / batch
+ *   q_len, k_len        device int32 [batch], or NULL: up to the next start.  Lengths and starts live on the device and are not
+ *                       checked: they are cut to the rows that there are, a length also to the next start
+ *   lse                 device fp32 [q_heads, q_rows]
+ * Rows of no sequence are neither read nor written (out, lse and the gradients keep what they held there).  A value that is not
+ * finite reaches only queries and keys that see it or lie in the same tile of up to 128.
+ * head_dim 32, 64 or 128; q_heads a multiple of kv_heads; q_rows * (q_heads / kv_heads) and k_rows < 2^31 - 2^20, and each of
+ * them / 32, plus batch, times kv_heads < 2^24; strides
+ * multiples of 16 bytes and at least heads * head_dim; pointers 16-byte aligned.  Outputs may not overlap inputs.
+ * workspace: mrem_attention_workspace_bytes(cfg, backward) bytes (0: may be NULL), not shared by calls that overlap in time; the
+ * contents carry nothing from call to call.
+ */
+typedef struct {
+  int32_t dtype; /* mrem_dtype */
+  int32_t batch, q_heads, kv_heads, head_dim;
+  int32_t causal, window; /* window 0: none */
+  float scale;            /* of the scores, positive; usually head_dim^-0.5 */
+  int64_t q_rows, k_rows;
+  int64_t ld_q, ld_k, ld_v, ld_out;
+} mrem_attention_config;
+size_t mrem_attention_workspace_bytes(const mrem_attention_config* cfg, int32_t backward); /* 0 also for sizes that are refused */
+mrem_status mrem_attention_forward(const mrem_attention_config* cfg, const void* q, const void* k, const void* v, const int32_t* q_start,
+                                   const int32_t* k_start, const int32_t* q_len, const int32_t* k_len, void* out, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* hip_stream);
+mrem_status mrem_attention_backward(const mrem_attention_config* cfg, const void* q, const void* k, const void* v, const void* out,
+                                    const float* lse, const void* d_out, const int32_t* q_start, const int32_t* k_start,
+                                    const int32_t* q_len, const int32_t* k_len, void* dq, void* dk, void* dv, void* workspace,
+                                    size_t workspace_bytes, void* hip_stream);
+
+/*
+ * mrem_distill_loss -- distillation from a teacher's top logits, with its gradient: for row t, student logits x over `vocab` tokens
+ * and the teacher's k pairs (token, logit z),
+ *   q = softmax(x / temperature),   p_i = exp(z_i / temperature) / sum over the listed tokens,
+ *   loss_t = sum_i p_i (log p_i - log q_i);
+ * with teacher_lse, the log-sum-exp of z / temperature over the teacher's whole vocabulary, p_i = exp(z_i / temperature - teacher_lse) and
+ * the rest r = max(0, 1 - sum p_i) is the probability of "any other token": loss_t += r (log r - log s), s = sum of q over the
+ * tokens not listed.  loss = scale * sum_t row_weight[t] loss_t (a factor temperature^2 is the caller's, in scale).
+ *   logits        device dtype [rows, vocab], rows ld elements apart
+ *   top_logits    device fp32 [rows, k]; top_index: device int32 [rows, k]; an index outside 0..vocab-1 marks an entry that is not
+ *                 there; a token listed twice counts with both probabilities
+ *   teacher_lse   device fp32 [rows] or NULL
+ *   row_weight    device fp32 [rows] or NULL (all 1); a row of weight 0 is not read: its loss and its gradient are 0
+ *   loss_rows     device fp32 [rows] (out), without weight and scale
+ *   loss_out      device fp32 [1] or NULL (out)
+ *   grad          device dtype [rows, vocab], rows ld_grad elements apart, or NULL (out): of loss with respect to logits; may be
+ *                 logits themselves (ld_grad = ld), and may not overlap them otherwise
+ * vocab 1..2^20, k 1..1024, temperature > 0, strides >= vocab.  Pointers need the alignment of their elements only.  rows = 0
+ * sets loss_out to 0; rows < 2^22.
+ */
+mrem_status mrem_distill_loss(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const float* top_logits,
+                              const int32_t* top_index, int32_t k, const float* teacher_lse, float temperature, const float* row_weight,
+                              float scale, float* loss_rows, float* loss_out, void* grad, int64_t ld_grad, void* hip_stream);
+
+/*
  * Non-finite detection.  mrem_set_nonfinite_flag gives the context a device int32 (caller-owned, cleared
  * by the caller; NULL switches the check off): every mrem_module_step on the context then sets it to 1
  * when its total loss is a NaN or infinite -- a non-finite value anywhere in a layer output reaches that

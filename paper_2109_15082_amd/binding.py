@@ -32,7 +32,9 @@ EXPORTS = ("mrem_create", "mrem_destroy", "mrem_last_error", "mrem_param_count",
            "mrem_module_forward", "mrem_module_forward_static", "mrem_static_scratch_bytes", "mrem_module_step", "mrem_rem_vector_count", "mrem_rem_workspace_bytes", "mrem_rem_step", "mrem_mix_inputs", "mrem_profile_gemm_begin",
            "mrem_profile_gemm_end", "mrem_profile_kernel_count", "mrem_profile_kernel_get", "mrem_set_nonfinite_flag", "mrem_check_nonfinite", "mrem_schedule_lr", "mrem_schedule_lambda",
            "mrem_queue_bytes", "mrem_queue_create", "mrem_queue_destroy", "mrem_queue_size", "mrem_queue_write_slot", "mrem_queue_push",
-           "mrem_queue_publish", "mrem_queue_entry")
+           "mrem_queue_publish", "mrem_queue_entry", "mrem_rotary_frequencies", "mrem_rotary_forward", "mrem_rotary_backward",
+           "mrem_attention_workspace_bytes", "mrem_attention_forward", "mrem_attention_backward", "mrem_distill_loss")
+MREM_ROTARY_PLAIN, MREM_ROTARY_LINEAR, MREM_ROTARY_BASE, MREM_ROTARY_BANDS = 0, 1, 2, 3
 
 
 class mrem_config(C.Structure):
@@ -41,6 +43,12 @@ class mrem_config(C.Structure):
                 ("act_dtype", C.c_int32), ("loss_layer_mask", C.c_uint32), ("loss_mean", C.c_int32),
                 ("ln_eps", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("adam_eps", C.c_float),
                 ("weight_decay", C.c_float), ("step_floor", C.c_float), ("per_channel", C.c_int32)]
+
+
+class mrem_attention_config(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("causal", C.c_int32), ("window", C.c_int32), ("scale", C.c_float), ("q_rows", C.c_int64), ("k_rows", C.c_int64),
+                ("ld_q", C.c_int64), ("ld_k", C.c_int64), ("ld_v", C.c_int64), ("ld_out", C.c_int64)]
 
 
 _vp, _i32, _i64, _f32, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
@@ -123,6 +131,19 @@ _lib.mrem_queue_publish.argtypes = [_vp]
 _lib.mrem_queue_publish.restype = C.c_int
 _lib.mrem_queue_entry.argtypes = [_vp, _i32, C.POINTER(_vp), C.POINTER(_vp), C.POINTER(_vp)]
 _lib.mrem_queue_entry.restype = C.c_int
+_lib.mrem_rotary_frequencies.argtypes = [_i32, C.c_double, _i32, C.c_double, C.c_double, C.c_double, C.c_double, _vp]
+_lib.mrem_rotary_frequencies.restype = C.c_int
+for _f in (_lib.mrem_rotary_forward, _lib.mrem_rotary_backward):
+    _f.argtypes = [_vp, _vp, _i32, _i64, _i32, _i32, _i64, _i64, _i32, _i32, _f32, _vp, _vp, _i64, _vp]
+    _f.restype = C.c_int
+_lib.mrem_attention_workspace_bytes.argtypes = [C.POINTER(mrem_attention_config), _i32]
+_lib.mrem_attention_workspace_bytes.restype = _sz
+_lib.mrem_attention_forward.argtypes = [C.POINTER(mrem_attention_config)] + [_vp] * 10 + [_sz, _vp]
+_lib.mrem_attention_forward.restype = C.c_int
+_lib.mrem_attention_backward.argtypes = [C.POINTER(mrem_attention_config)] + [_vp] * 14 + [_sz, _vp]
+_lib.mrem_attention_backward.restype = C.c_int
+_lib.mrem_distill_loss.argtypes = [_vp, _i32, _i64, _i64, _i64, _vp, _vp, _i32, _vp, _f32, _vp, _f32, _vp, _vp, _vp, _i64, _vp]
+_lib.mrem_distill_loss.restype = C.c_int
 
 
 class MremError(RuntimeError):
@@ -346,6 +367,161 @@ def mrem_queue_publish(q) -> None:
 def mrem_queue_entry(q, age: int):
     """Device addresses (fp half, quantized half, lengths or None) of the entry of that age (0 = newest)."""
     return _three(_lib.mrem_queue_entry, q, age)
+
+
+# ------------------------------------------------------------------------------
+# operators outside the module step.  Sizes, strides and types come from the tensors, whose fit is checked here: the C
+# functions see addresses only.  Work goes to the current stream of the tensors' device (or to `stream`).
+# ------------------------------------------------------------------------------
+
+_DTYPES = {torch.bfloat16: MREM_BF16, torch.float32: MREM_FP32}
+
+
+def _fit(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _heads(t: torch.Tensor, name: str) -> int:
+    """Address of a [rows, heads, head_dim] view whose heads are contiguous; rows may lie any distance apart."""
+    _fit(t.dim() == 3 and t.dtype in _DTYPES, f"{name}: bf16 or fp32 [rows, heads, head_dim] expected")
+    _fit(t.numel() == 0 or ((t.stride(2) == 1 or t.shape[2] == 1) and (t.stride(1) == t.shape[2] or t.shape[1] == 1)), f"{name}: the heads of a row must be contiguous")
+    return t.data_ptr() or None
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    """Elements between rows; of a single row or none, its width."""
+    return t.stride(0) if t.shape[0] > 1 else t[0].numel() if t.shape[0] else t.shape[1:].numel()
+
+
+def _plain(t: Optional[torch.Tensor], name: str, dtype, shape) -> Optional[int]:
+    if t is None:
+        return None
+    _fit(t.dtype == dtype and tuple(t.shape) == tuple(shape), f"{name}: {dtype} {tuple(shape)} expected, got {t.dtype} {tuple(t.shape)}")
+    _fit(t.is_contiguous(), f"{name}: contiguous tensor required")
+    return t.data_ptr() or None
+
+
+class _on:
+    """The device that all the tensors are on is the current one inside; gives the stream for it."""
+
+    def __init__(self, stream, *tensors):
+        devices = {t.device for t in tensors if t is not None}
+        _fit(len(devices) == 1, f"the tensors are on several devices: {sorted(map(str, devices))}")
+        (self.device,) = devices
+        _fit(self.device.type == "cuda", "device tensors required")
+        self.stream = stream
+        self.guard = None
+
+    def __enter__(self):
+        if self.device.index != torch.cuda.current_device():
+            self.guard = torch.cuda.device(self.device)
+            self.guard.__enter__()
+        return _stream(self.stream)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def mrem_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int = MREM_ROTARY_PLAIN, factor: float = 1.0,
+                            trained: float = 4096.0, fast: float = 32.0, slow: float = 1.0) -> torch.Tensor:
+    """fp64 [rotary_dim / 2] on the host; the calls below want it on the device."""
+    freq = torch.empty(max(int(rotary_dim), 0) // 2, dtype=torch.float64)
+    _check(_lib.mrem_rotary_frequencies(rotary_dim, base, scaling, factor, trained, fast, slow, freq.data_ptr() or None))
+    return freq
+
+
+def _rotary(fn, x, y, rotary_dim, interleaved, amplitude, freq, positions, seq, stream):
+    xp, yp = _heads(x, "x"), _heads(y, "y")
+    _fit(x.shape == y.shape and x.dtype == y.dtype, "x and y must have one shape and type")
+    fp = _plain(freq, "freq", torch.float64, (rotary_dim // 2,))
+    pp = _plain(positions, "positions", torch.int32, (x.shape[0],))
+    with _on(stream, x, y, freq, positions) as st:
+        _check(fn(xp, yp, _DTYPES[x.dtype], x.shape[0], x.shape[1], x.shape[2], _row_stride(x), _row_stride(y), rotary_dim, int(interleaved),
+                  amplitude, fp, pp, x.shape[0] or 1 if seq is None else seq, st))
+
+
+def mrem_rotary_forward(x, y, rotary_dim, interleaved, amplitude, freq, positions=None, seq=None, stream=None) -> None:
+    """x, y: [rows, heads, head_dim]; seq: rows of a sequence where there are no positions (None: all are one)."""
+    _rotary(_lib.mrem_rotary_forward, x, y, rotary_dim, interleaved, amplitude, freq, positions, seq, stream)
+
+
+def mrem_rotary_backward(dy, dx, rotary_dim, interleaved, amplitude, freq, positions=None, seq=None, stream=None) -> None:
+    _rotary(_lib.mrem_rotary_backward, dy, dx, rotary_dim, interleaved, amplitude, freq, positions, seq, stream)
+
+
+def attention_config(q, k, v, out, batch: int, causal: int = 0, window: int = 0, scale: Optional[float] = None) -> mrem_attention_config:
+    """The config of calls on tensors like these ([rows, heads, head_dim]); scale: head_dim^-0.5 if None."""
+    for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
+        _heads(t, name)
+        _fit(t.dtype == q.dtype and t.shape[2] == q.shape[2], f"{name}: q's type and head_dim expected")
+    _fit(k.shape == v.shape and q.shape == out.shape, "k and v, and q and out, must have one shape")
+    return mrem_attention_config(dtype=_DTYPES[q.dtype], batch=batch, q_heads=q.shape[1], kv_heads=k.shape[1], head_dim=q.shape[2],
+                                 causal=int(causal), window=window, scale=q.shape[2] ** -0.5 if scale is None else scale, q_rows=q.shape[0],
+                                 k_rows=k.shape[0], ld_q=_row_stride(q), ld_k=_row_stride(k), ld_v=_row_stride(v), ld_out=_row_stride(out))
+
+
+def mrem_attention_workspace_bytes(cfg, backward) -> int:
+    return _lib.mrem_attention_workspace_bytes(C.byref(cfg), int(bool(backward)))
+
+
+def _attention_tensor(cfg, t, name, rows, heads, ld):
+    p = _heads(t, name)
+    _fit(_DTYPES[t.dtype] == cfg.dtype and tuple(t.shape) == (rows, heads, cfg.head_dim), f"{name}: another type or shape than the config's")
+    _fit(t.shape[0] <= 1 or t.stride(0) == ld, f"{name}: rows {ld} elements apart expected")
+    return p
+
+
+def _attention_sequences(cfg, q_start, k_start, q_len, k_len):
+    n = cfg.batch
+    return [_plain(t, name, torch.int32, (m,)) for t, name, m in ((q_start, "q_start", n + 1), (k_start, "k_start", n + 1), (q_len, "q_len", n), (k_len, "k_len", n))]
+
+
+def _workspace(t):
+    return (None, 0) if t is None else (_ptr(t) or None, t.numel() * t.element_size())
+
+
+def mrem_attention_forward(cfg, q, k, v, q_start, k_start, q_len, k_len, out, lse, workspace, stream=None) -> None:
+    qs, ks = (cfg.q_rows, cfg.q_heads), (cfg.k_rows, cfg.kv_heads)
+    ptrs = [_attention_tensor(cfg, q, "q", *qs, cfg.ld_q), _attention_tensor(cfg, k, "k", *ks, cfg.ld_k), _attention_tensor(cfg, v, "v", *ks, cfg.ld_v)]
+    outs = [_attention_tensor(cfg, out, "out", *qs, cfg.ld_out), _plain(lse, "lse", torch.float32, (cfg.q_heads, cfg.q_rows))]
+    seqs = _attention_sequences(cfg, q_start, k_start, q_len, k_len)
+    with _on(stream, q, k, v, q_start, k_start, q_len, k_len, out, lse, workspace) as st:
+        _check(_lib.mrem_attention_forward(C.byref(cfg), *ptrs, *seqs, *outs, *_workspace(workspace), st))
+
+
+def mrem_attention_backward(cfg, q, k, v, out, lse, d_out, q_start, k_start, q_len, k_len, dq, dk, dv, workspace, stream=None) -> None:
+    qs, ks = (cfg.q_rows, cfg.q_heads), (cfg.k_rows, cfg.kv_heads)
+    ptrs = [_attention_tensor(cfg, q, "q", *qs, cfg.ld_q), _attention_tensor(cfg, k, "k", *ks, cfg.ld_k), _attention_tensor(cfg, v, "v", *ks, cfg.ld_v),
+            _attention_tensor(cfg, out, "out", *qs, cfg.ld_out), _plain(lse, "lse", torch.float32, (cfg.q_heads, cfg.q_rows)),
+            _attention_tensor(cfg, d_out, "d_out", *qs, cfg.ld_out)]
+    outs = [_attention_tensor(cfg, dq, "dq", *qs, cfg.ld_q), _attention_tensor(cfg, dk, "dk", *ks, cfg.ld_k), _attention_tensor(cfg, dv, "dv", *ks, cfg.ld_v)]
+    seqs = _attention_sequences(cfg, q_start, k_start, q_len, k_len)
+    with _on(stream, q, k, v, out, lse, d_out, q_start, k_start, q_len, k_len, dq, dk, dv, workspace) as st:
+        _check(_lib.mrem_attention_backward(C.byref(cfg), *ptrs, *seqs, *outs, *_workspace(workspace), st))
+
+
+def _logits(t, name):
+    _fit(t.dim() == 2 and t.dtype in _DTYPES and (t.stride(1) == 1 or t.shape[1] == 1), f"{name}: bf16 or fp32 [rows, vocab] with contiguous rows expected")
+    return t.data_ptr() or None
+
+
+def mrem_distill_loss(logits, top_logits, top_index, teacher_lse, temperature, row_weight, scale, loss_rows, loss_out, grad, stream=None) -> None:
+    """logits, grad: [rows, vocab], rows any distance apart; teacher_lse, row_weight, loss_out and grad may be None."""
+    xp = _logits(logits, "logits")
+    rows, vocab = logits.shape
+    _fit(top_logits.dim() == 2, "top_logits: [rows, k] expected")
+    k = top_logits.shape[1]
+    gp, ld_grad = None, vocab
+    if grad is not None:
+        gp, ld_grad = _logits(grad, "grad"), _row_stride(grad)
+        _fit(grad.shape == logits.shape and grad.dtype == logits.dtype, "grad: the logits' shape and type expected")
+    args = [_plain(top_logits, "top_logits", torch.float32, (rows, k)), _plain(top_index, "top_index", torch.int32, (rows, k)), k,
+            _plain(teacher_lse, "teacher_lse", torch.float32, (rows,)), temperature, _plain(row_weight, "row_weight", torch.float32, (rows,)), scale,
+            _plain(loss_rows, "loss_rows", torch.float32, (rows,)), _plain(loss_out, "loss_out", torch.float32, (1,))]
+    with _on(stream, logits, top_logits, top_index, teacher_lse, row_weight, loss_rows, loss_out, grad) as st:
+        _check(_lib.mrem_distill_loss(xp, _DTYPES[logits.dtype], rows, vocab, _row_stride(logits), *args, gp, ld_grad, st))
 
 
 # ------------------------------------------------------------------------------

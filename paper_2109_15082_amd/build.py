@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libmrem.so")
 OBJ_DIR = os.path.join(HERE, "_build")
-SOURCES = ["mrem_api.hip", "mrem_elem.hip", "mrem_gemm.hip", "mrem_attn.hip", "mrem_attn_mfma.hip"]
+SOURCES = ["mrem_api.hip", "mrem_elem.hip", "mrem_gemm.hip", "mrem_attn.hip", "mrem_attn_mfma.hip", "mrem_rotary.hip", "mrem_distill.hip",
+           "mrem_seq_attn.hip"]
 # the products' kernels take longest to compile: one unit for each operand form of mrem_gemm.hip, and the rest of it
 PARTS = {"mrem_gemm.hip": [0, 1, 2, 3, 4]}
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",

@@ -1411,6 +1411,190 @@ extern "C" mrem_status mrem_mix_inputs(mrem_ctx* ctx, const void* x_fp, const vo
   return finish(ctx, "mrem_mix_inputs");
 }
 
+// ---- operators outside the module step ---------------------------------------------
+
+static bool known_dtype(int32_t dtype) { return dtype == MREM_BF16 || dtype == MREM_FP32; }
+static int dt_of(int32_t dtype) { return dtype == MREM_BF16 ? DT_BF16 : DT_F32; }
+
+extern "C" mrem_status mrem_rotary_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double trained,
+                                               double fast, double slow, double* freq) {
+  const char* who = "mrem_rotary_frequencies";
+  if (!freq) return fail(nullptr, MREM_EINVAL, std::string(who) + ": freq is null");
+  if (rotary_dim < 2 || rotary_dim % 2) return fail(nullptr, MREM_ESHAPE, std::string(who) + ": rotary_dim must be even, >= 2");
+  if (scaling < MREM_ROTARY_PLAIN || scaling > MREM_ROTARY_BANDS) return fail(nullptr, MREM_EINVAL, std::string(who) + ": unknown scaling");
+  const auto good = [](double v) { return v > 0 && std::isfinite(v); };
+  if (!good(base)) return fail(nullptr, MREM_EINVAL, std::string(who) + ": base must be positive");
+  if (scaling != MREM_ROTARY_PLAIN && !good(factor)) return fail(nullptr, MREM_EINVAL, std::string(who) + ": factor must be positive");
+  if (scaling == MREM_ROTARY_BANDS && !(good(trained) && std::isfinite(fast) && std::isfinite(slow) && fast > slow))
+    return fail(nullptr, MREM_EINVAL, std::string(who) + ": trained must be positive and fast above slow");
+  if (scaling == MREM_ROTARY_BASE && rotary_dim > 2) base *= std::pow(factor, rotary_dim / (rotary_dim - 2.0));
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / rotary_dim);
+    if (scaling == MREM_ROTARY_LINEAR) f /= factor;
+    if (scaling == MREM_ROTARY_BANDS) {
+      const double turns = trained * f / (2 * 3.14159265358979323846);
+      const double keep = std::min(std::max((turns - slow) / (fast - slow), 0.0), 1.0);
+      f = keep * f + (1 - keep) * f / factor;
+    }
+    freq[i] = f;
+  }
+  return MREM_OK;
+}
+
+static mrem_status rotary_call(const char* who, const void* x, void* y, int32_t dtype, int64_t rows, int32_t heads, int32_t head_dim,
+                               int64_t ld_x, int64_t ld_y, int32_t rotary_dim, int32_t interleaved, float amplitude, float sign,
+                               const double* freq, const int32_t* positions, int64_t seq, void* hip_stream) {
+  const mrem_ctx* ctx = nullptr;
+  if (!known_dtype(dtype)) return fail(nullptr, MREM_EINVAL, std::string(who) + ": dtype must be MREM_BF16 or MREM_FP32");
+  if (rows < 0 || rows >= (int64_t)1 << 31) return fail(nullptr, MREM_ESHAPE, std::string(who) + ": rows must be in 0..2^31-1");
+  if (head_dim < 1 || head_dim > 512) return fail(nullptr, MREM_ESHAPE, std::string(who) + ": head_dim must be in 1..512");
+  if (heads < 1 || heads > 1 << 16) return fail(nullptr, MREM_ESHAPE, std::string(who) + ": heads must be in 1..65536");
+  if (rotary_dim < 2 || rotary_dim % 2 || rotary_dim > head_dim) return fail(nullptr, MREM_ESHAPE, std::string(who) + ": rotary_dim must be even, in 2..head_dim");
+  const int64_t width = (int64_t)heads * head_dim;
+  if (ld_x < width || ld_y < width) return fail(nullptr, MREM_ESHAPE, std::string(who) + ": rows overlap: stride below heads * head_dim");
+  if (interleaved != 0 && interleaved != 1) return fail(nullptr, MREM_EINVAL, std::string(who) + ": interleaved must be 0 or 1");
+  if (!positions && seq < 1) return fail(nullptr, MREM_ESHAPE, std::string(who) + ": seq must be >= 1 without positions");
+  if (rows == 0) return MREM_OK;
+  REQUIRE_PTR(x, who);
+  REQUIRE_PTR(y, who);
+  if (x == y && ld_x != ld_y) return fail(nullptr, MREM_EINVAL, std::string(who) + ": in place needs one stride");
+  if (!freq || (reinterpret_cast<uintptr_t>(freq) & 7u)) return fail(nullptr, MREM_EINVAL, std::string(who) + ": freq is null or misaligned");
+  if (reinterpret_cast<uintptr_t>(positions) & 3u) return fail(nullptr, MREM_EINVAL, std::string(who) + ": positions are misaligned");
+  rotary(dt_of(dtype), x, y, rows, heads, head_dim, ld_x, ld_y, rotary_dim, interleaved != 0, amplitude, sign, freq, positions, seq, (hipStream_t)hip_stream);
+  return finish(nullptr, who);
+}
+extern "C" mrem_status mrem_rotary_forward(const void* x, void* y, int32_t dtype, int64_t rows, int32_t heads, int32_t head_dim, int64_t ld_x,
+                                           int64_t ld_y, int32_t rotary_dim, int32_t interleaved, float amplitude, const double* freq,
+                                           const int32_t* positions, int64_t seq, void* hip_stream) {
+  return rotary_call("mrem_rotary_forward", x, y, dtype, rows, heads, head_dim, ld_x, ld_y, rotary_dim, interleaved, amplitude, 1.f, freq, positions, seq, hip_stream);
+}
+extern "C" mrem_status mrem_rotary_backward(const void* dy, void* dx, int32_t dtype, int64_t rows, int32_t heads, int32_t head_dim, int64_t ld_dy,
+                                            int64_t ld_dx, int32_t rotary_dim, int32_t interleaved, float amplitude, const double* freq,
+                                            const int32_t* positions, int64_t seq, void* hip_stream) {
+  return rotary_call("mrem_rotary_backward", dy, dx, dtype, rows, heads, head_dim, ld_dy, ld_dx, rotary_dim, interleaved, amplitude, -1.f, freq, positions, seq, hip_stream);
+}
+
+static mrem_status attention_shape(const char* who, const mrem_attention_config* cfg, SeqAttn* a) {
+  if (!cfg) return fail(nullptr, MREM_EINVAL, std::string(who) + ": null config");
+  const mrem_attention_config& c = *cfg;
+  const auto bad = [&](mrem_status st, const char* what) { return fail(nullptr, st, std::string(who) + ": " + what); };
+  if (!known_dtype(c.dtype)) return bad(MREM_EINVAL, "dtype must be MREM_BF16 or MREM_FP32");
+  if (c.head_dim != 32 && c.head_dim != 64 && c.head_dim != 128) return bad(MREM_ESHAPE, "head_dim must be 32, 64 or 128");
+  if (c.kv_heads < 1 || c.q_heads < 1 || c.q_heads % c.kv_heads || c.q_heads > 1 << 16) return bad(MREM_ESHAPE, "q_heads must be a multiple of kv_heads, <= 65536");
+  if (c.batch < 1 || c.batch > 1 << 20) return bad(MREM_ESHAPE, "batch must be in 1..2^20");
+  if (c.causal != 0 && c.causal != 1) return bad(MREM_EINVAL, "causal must be 0 or 1");
+  if (c.window < 0 || (c.window && !c.causal)) return bad(MREM_EINVAL, "window must be >= 0, and 0 unless causal");
+  if (!(c.scale > 0.f) || !std::isfinite(c.scale)) return bad(MREM_EINVAL, "scale must be positive");
+  const int64_t most = ((int64_t)1 << 31) - ((int64_t)1 << 20), group = c.q_heads / c.kv_heads;
+  if (c.q_rows < 0 || c.k_rows < 0 || c.q_rows >= most || c.q_rows * group >= most || c.k_rows >= most) return bad(MREM_ESHAPE, "too many rows");
+  // a block of 256 threads takes 32 rows or more of a key head: a launch has fewer than 2^32 threads
+  if ((c.q_rows * group / 32 + c.batch) * c.kv_heads >= (int64_t)1 << 24 || (c.k_rows / 32 + c.batch) * c.kv_heads >= (int64_t)1 << 24)
+    return bad(MREM_ESHAPE, "too many rows times heads");
+  const int64_t piece = 16 / (int64_t)dt_size(dt_of(c.dtype)), limit = (int64_t)1 << 40;
+  for (int64_t ld : {c.ld_q, c.ld_k, c.ld_v, c.ld_out})
+    if (ld % piece || ld > limit) return bad(MREM_ESHAPE, "strides must be multiples of 16 bytes");
+  if (c.ld_q < (int64_t)c.q_heads * c.head_dim || c.ld_out < (int64_t)c.q_heads * c.head_dim || c.ld_k < (int64_t)c.kv_heads * c.head_dim ||
+      c.ld_v < (int64_t)c.kv_heads * c.head_dim)
+    return bad(MREM_ESHAPE, "rows overlap: stride below heads * head_dim");
+  *a = SeqAttn{};
+  a->dt = dt_of(c.dtype); a->batch = c.batch; a->hq = c.q_heads; a->hk = c.kv_heads; a->d = c.head_dim;
+  a->causal = c.causal; a->window = c.window; a->scale = c.scale;
+  a->q_rows = c.q_rows; a->k_rows = c.k_rows; a->ld_q = c.ld_q; a->ld_k = c.ld_k; a->ld_v = c.ld_v; a->ld_o = c.ld_out;
+  return MREM_OK;
+}
+static mrem_status attention_sequences(const char* who, SeqAttn* a, const int32_t* q_start, const int32_t* k_start, const int32_t* q_len,
+                                       const int32_t* k_len, const void* workspace, size_t have, size_t need) {
+  for (const int32_t* p : {q_start, k_start, q_len, k_len})
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(nullptr, MREM_EINVAL, std::string(who) + ": starts or lengths are misaligned");
+  if ((!q_start && a->q_rows % a->batch) || (!k_start && a->k_rows % a->batch))
+    return fail(nullptr, MREM_ESHAPE, std::string(who) + ": without starts the rows must be a multiple of batch");
+  if (need && (!workspace || !aligned16(workspace))) return fail(nullptr, MREM_EINVAL, std::string(who) + ": workspace null or misaligned");
+  if (have < need) return fail(nullptr, MREM_EWORKSPACE, std::string(who) + ": workspace too small");
+  a->q_start = q_start; a->k_start = k_start; a->q_len = q_len; a->k_len = k_len;
+  return MREM_OK;
+}
+extern "C" size_t mrem_attention_workspace_bytes(const mrem_attention_config* cfg, int32_t backward) {
+  SeqAttn a;
+  if (attention_shape("mrem_attention_workspace_bytes", cfg, &a) != MREM_OK) return 0;
+  const size_t f = seq_attn_fwd_bytes(a);
+  return backward ? std::max(f, seq_attn_bwd_bytes(a)) : f;
+}
+extern "C" mrem_status mrem_attention_forward(const mrem_attention_config* cfg, const void* q, const void* k, const void* v,
+                                              const int32_t* q_start, const int32_t* k_start, const int32_t* q_len, const int32_t* k_len,
+                                              void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const char* who = "mrem_attention_forward";
+  const mrem_ctx* ctx = nullptr;
+  SeqAttn a;
+  if (const mrem_status st = attention_shape(who, cfg, &a)) return st;
+  if (const mrem_status st = attention_sequences(who, &a, q_start, k_start, q_len, k_len, workspace, workspace_bytes, seq_attn_fwd_bytes(a))) return st;
+  if (a.q_rows == 0) return MREM_OK;
+  REQUIRE_PTR(q, who);
+  REQUIRE_PTR(out, who);
+  REQUIRE_PTR(lse, who);
+  if (a.k_rows) {
+    REQUIRE_PTR(k, who);
+    REQUIRE_PTR(v, who);
+  }
+  a.q = q; a.k = k; a.v = v; a.out = out; a.lse = lse;
+  seq_attn_fwd(a, workspace, (hipStream_t)hip_stream);
+  return finish(nullptr, who);
+}
+extern "C" mrem_status mrem_attention_backward(const mrem_attention_config* cfg, const void* q, const void* k, const void* v, const void* out,
+                                               const float* lse, const void* d_out, const int32_t* q_start, const int32_t* k_start,
+                                               const int32_t* q_len, const int32_t* k_len, void* dq, void* dk, void* dv, void* workspace,
+                                               size_t workspace_bytes, void* hip_stream) {
+  const char* who = "mrem_attention_backward";
+  const mrem_ctx* ctx = nullptr;
+  SeqAttn a;
+  if (const mrem_status st = attention_shape(who, cfg, &a)) return st;
+  if (const mrem_status st = attention_sequences(who, &a, q_start, k_start, q_len, k_len, workspace, workspace_bytes, seq_attn_bwd_bytes(a))) return st;
+  if (a.q_rows == 0 && a.k_rows == 0) return MREM_OK;
+  if (a.q_rows) {
+    REQUIRE_PTR(q, who);
+    REQUIRE_PTR(out, who);
+    REQUIRE_PTR(lse, who);
+    REQUIRE_PTR(d_out, who);
+    REQUIRE_PTR(dq, who);
+  }
+  if (a.k_rows) {
+    REQUIRE_PTR(k, who);
+    REQUIRE_PTR(v, who);
+    REQUIRE_PTR(dk, who);
+    REQUIRE_PTR(dv, who);
+  }
+  a.q = q; a.k = k; a.v = v; a.out = const_cast<void*>(out); a.lse = const_cast<float*>(lse);
+  a.dout = d_out; a.dq = dq; a.dk = dk; a.dv = dv;
+  seq_attn_bwd(a, workspace, (hipStream_t)hip_stream);
+  return finish(nullptr, who);
+}
+
+extern "C" mrem_status mrem_distill_loss(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const float* top_logits,
+                                         const int32_t* top_index, int32_t k, const float* teacher_lse, float temperature,
+                                         const float* row_weight, float scale, float* loss_rows, float* loss_out, void* grad,
+                                         int64_t ld_grad, void* hip_stream) {
+  const auto bad = [](mrem_status st, const char* what) { return fail(nullptr, st, std::string("mrem_distill_loss: ") + what); };
+  if (!known_dtype(dtype)) return bad(MREM_EINVAL, "dtype must be MREM_BF16 or MREM_FP32");
+  if (rows < 0 || rows >= (int64_t)1 << 22) return bad(MREM_ESHAPE, "rows must be in 0..2^22-1");  // a block of up to 1024 threads each
+  if (vocab < 1 || vocab > kDistillMaxVocab) return bad(MREM_ESHAPE, "vocab must be in 1..2^20");
+  if (k < 1 || k > kDistillMaxK) return bad(MREM_ESHAPE, "k must be in 1..1024");
+  if (ld < vocab || (grad && ld_grad < vocab)) return bad(MREM_ESHAPE, "rows overlap: stride below vocab");
+  if (!(temperature > 0.f) || !std::isfinite(temperature)) return bad(MREM_EINVAL, "temperature must be positive");
+  if (!std::isfinite(scale)) return bad(MREM_EINVAL, "scale must be finite");
+  const uintptr_t part = dt_size(dt_of(dtype)) - 1;
+  if ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(grad)) & part) return bad(MREM_EINVAL, "logits or grad are misaligned");
+  for (const void* p : {(const void*)top_logits, (const void*)top_index, (const void*)teacher_lse, (const void*)row_weight, (const void*)loss_rows, (const void*)loss_out})
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return bad(MREM_EINVAL, "a pointer is misaligned");
+  if (rows && (!logits || !top_logits || !top_index || !loss_rows)) return bad(MREM_EINVAL, "logits, top_logits, top_index or loss_rows is null");
+  if (grad && grad == logits && ld_grad != ld) return bad(MREM_EINVAL, "in place needs one stride");
+  if (rows == 0 && !loss_out) return MREM_OK;
+  DistillArg a;
+  a.x = logits; a.grad = grad; a.rows = rows; a.ld = ld; a.ld_grad = ld_grad; a.vocab = (int)vocab; a.k = k;
+  a.top = top_logits; a.index = top_index; a.teacher_lse = teacher_lse; a.weight = row_weight;
+  a.temperature = temperature; a.scale = scale; a.loss_rows = loss_rows; a.loss_out = loss_out;
+  distill_loss(dt_of(dtype), a, (hipStream_t)hip_stream);
+  return finish(nullptr, "mrem_distill_loss");
+}
+
 extern "C" mrem_status mrem_profile_gemm_begin(mrem_ctx* ctx) {
   if (!ctx) return fail(nullptr, MREM_EINVAL, "mrem_profile_gemm_begin: null context");
   gemm_profile_begin(&ctx->prof);

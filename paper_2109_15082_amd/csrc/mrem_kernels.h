@@ -317,4 +317,42 @@ void adam_vector(float* p, const float* g, float* m, float* v, const VecJob* job
 // both jobs have len = 1; behind `grad` AdamW without decay on the scalar p, which keeps the lower bound
 void reduce_and_step(const ReduceJob& other, const ReduceJob& grad, float* p, float* m, float* v, AdamArg a, hipStream_t st);
 
+// ---- operators outside the module step ---------------------------------------------
+// sign: +1 forward, -1 the transposed rotation.
+void rotary(int dt, const void* x, void* y, int64_t rows, int heads, int dim, int64_t ld_x, int64_t ld_y, int rotary_dim, bool interleaved,
+            float amplitude, float sign, const double* freq, const int32_t* positions, int64_t seq, hipStream_t st);
+
+// Tensors and sequences of one attention call; see the header of the ABI.
+struct SeqAttn {
+  int dt, batch, hq, hk, d, causal, window;
+  float scale;
+  int64_t q_rows, k_rows, ld_q, ld_k, ld_v, ld_o;
+  const void *q, *k, *v, *dout;
+  void *out, *dq, *dk, *dv;
+  float *lse, *delta;  // [hq, q_rows]
+  const int32_t *q_start, *k_start, *q_len, *k_len;
+  float* part;  // partial results of keys shared out among blocks
+  int splits;
+};
+size_t seq_attn_fwd_bytes(const SeqAttn& a);
+size_t seq_attn_bwd_bytes(const SeqAttn& a);
+void seq_attn_fwd(SeqAttn a, void* workspace, hipStream_t st);
+void seq_attn_bwd(SeqAttn a, void* workspace, hipStream_t st);
+
+constexpr int kDistillMaxK = 1024;
+constexpr int kDistillMaxVocab = 1 << 20;
+struct DistillArg {
+  const void* x;
+  void* grad;
+  int64_t rows, ld, ld_grad;
+  int vocab, k;
+  const float* top;
+  const int32_t* index;
+  const float* teacher_lse;
+  const float* weight;
+  float temperature, scale;
+  float *loss_rows, *loss_out;
+};
+void distill_loss(int dt, const DistillArg& a, hipStream_t st);
+
 }  // namespace mrem

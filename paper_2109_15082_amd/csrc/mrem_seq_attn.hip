@@ -1,0 +1,691 @@
+// Softmax attention over sequences of any lengths, with its gradients: causal or not, with a window, with shared key heads.
+//
+// Layout as in the module's attention kernels: score tiles are formed transposed, D[key][query] = K Q^T, so that in the 32x32
+// accumulator layout a lane owns one query (lane % 32) and 16 of a tile's 32 keys.  The softmax statistics of a query need one exchange
+// between lane halves, and the probabilities already have the layout of the second product's operand, O^T = V^T P^T, whose
+// V^T fragments come from the row-major tile by transposing LDS reads.  The kernel of the key gradients mirrors it: a lane owns a key.
+//
+// Rows.  The query heads of a key head read the same keys, so the queries of a key head are numbered (token, head) with the head
+// fastest and tiled as one axis: a token's `group` queries are neighbours, a key tile serves all of them, and a single token
+// fills `group` of a tile's rows instead of one in each of `group` tiles.
+// Sequences.  Tile slots are given out without knowing the lengths on the host: a sequence whose first row is s has the slots from
+// s / tile + b on, of which at least ceil(length / tile) lie before the next sequence's first; slots behind a sequence's tiles end at once.
+//
+// The matrix instructions and the vector-ALU work of the softmax bound the long cases, memory the single tokens.
+#include "mrem_common.h"
+#include "mrem_kernels.h"
+
+#include <algorithm>
+
+namespace mrem {
+
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr int kThreads = 256, kWaves = 4;
+
+// elements of a row of an LDS tile: 16 bytes more than the row, so that neither row nor column reads meet in a bank
+template <class T, int D>
+constexpr int kStride = D + 16 / (int)sizeof(T);
+
+// ---- fragments: 8 values a lane, contraction index 8 (lane / 32) + i ---------
+template <class T>
+struct Frag;
+template <>
+struct Frag<bf16_t> { bf16x8_t v; };
+template <>
+struct Frag<float> { float v[8]; };
+
+__device__ __forceinline__ f32x16_t mma(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16_t mma(const Frag<float>& a, const Frag<float>& b, f32x16_t c) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[i], b.v[i], c, 0, 0, 0);
+  return c;
+}
+__device__ __forceinline__ f32x16_t zero16() {
+  f32x16_t z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+// row (of 32) that accumulator register r of a lane in half h holds
+__device__ __forceinline__ int row_of(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+template <class T>
+__device__ __forceinline__ Frag<T> zero_frag() {
+  Frag<T> f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f.v[i] = static_cast<T>(0.f);
+  return f;
+}
+// 8 consecutive values (16-byte aligned)
+template <class T>
+__device__ __forceinline__ Frag<T> load8(const T* p) {
+  Frag<T> f;
+  if constexpr (sizeof(T) == 2) {
+    f.v = *reinterpret_cast<const bf16x8_t*>(p);
+  } else {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    f.v[0] = a.x; f.v[1] = a.y; f.v[2] = a.z; f.v[3] = a.w;
+    f.v[4] = b.x; f.v[5] = b.y; f.v[6] = b.z; f.v[7] = b.w;
+  }
+  return f;
+}
+// fragment down the rows of an LDS tile: column c0 + lane % 32, rows first + 0..3 and second + 0..3
+template <class T, int D>
+__device__ __forceinline__ Frag<T> load_cols(const T* tile, int c0, int first, int second, int lane) {
+  Frag<T> f;
+  if constexpr (sizeof(T) == 2) {
+    const int g = lane >> 4, s = lane & 15;
+    const T* p = tile + (s >> 2) * kStride<T, D> + c0 + 16 * (g & 1) + 4 * (s & 3);
+    union { bf16x8_t v; s16x4_t h[2]; } u;
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p + first * kStride<T, D>));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p + second * kStride<T, D>));
+    f.v = u.v;
+  } else {
+    const T* p = tile + c0 + (lane & 31);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f.v[i] = p[(first + i) * kStride<T, D>];
+      f.v[4 + i] = p[(second + i) * kStride<T, D>];
+    }
+  }
+  return f;
+}
+// accumulator registers 8 s .. 8 s + 7 as an operand.  bf16: probabilities and score gradients are rounded once, to 8 bits of
+// mantissa, as the values of the products around them are; what is added up stays in 32 bits
+template <class T>
+__device__ __forceinline__ Frag<T> from_acc(const f32x16_t& a, int s) {
+  Frag<T> f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f.v[i] = static_cast<T>(a[8 * s + i]);
+  return f;
+}
+// 32 x 32 tile: LDS rows [row0, row0 + 32) times the 32 rows held as fragments
+template <class T, int D>
+__device__ __forceinline__ f32x16_t rows_times(const T* tile, int row0, int lane, const Frag<T> (&b)[D / 16]) {
+  f32x16_t acc = zero16();
+  const T* p = tile + (row0 + (lane & 31)) * kStride<T, D> + (lane >> 5) * 8;
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) acc = mma(load8(p + 16 * kk), b[kk], acc);
+  return acc;
+}
+// acc[e][.] += sum over the tile's 32 rows of tile[row][e] w[row], w in accumulator order
+template <class T, int D>
+__device__ __forceinline__ void add_rows(f32x16_t (&acc)[D / 32], const T* tile, int row0, int lane, const f32x16_t& w) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const Frag<T> f = from_acc<T>(w, s);
+    const int r = row0 + 16 * s + 4 * (lane >> 5);
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) acc[e] = mma(load_cols<T, D>(tile, 32 * e, r, r + 8, lane), f, acc[e]);
+  }
+}
+// the other half wavefront's value
+__device__ __forceinline__ float other_half(float v) {
+  const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? x[0] : x[1]);
+}
+
+// ---- sequences ---------------------------------------------------------------
+struct Seq {
+  int64_t q0, k0;  // first rows
+  int qn, kn;
+};
+__device__ __forceinline__ int64_t start_of(const int32_t* start, int64_t rows, int batch, int b) {
+  return start ? min(max((int64_t)start[b], (int64_t)0), rows) : (rows / batch) * b;
+}
+__device__ __forceinline__ void sequence_rows(const int32_t* start, const int32_t* len, int64_t rows, int batch, int b, int64_t* first, int* n) {
+  const int64_t lo = start_of(start, rows, batch, b), hi = max(start_of(start, rows, batch, b + 1), lo);
+  const int64_t m = len ? min(max((int64_t)len[b], (int64_t)0), hi - lo) : hi - lo;
+  // the same for the whole block: kept in scalar registers
+  *first = ((int64_t)__builtin_amdgcn_readfirstlane((int)(lo >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)lo);
+  *n = __builtin_amdgcn_readfirstlane((int)m);
+}
+__device__ __forceinline__ Seq sequence(const SeqAttn& a, int b) {
+  Seq s;
+  sequence_rows(a.q_start, a.q_len, a.q_rows, a.batch, b, &s.q0, &s.qn);
+  sequence_rows(a.k_start, a.k_len, a.k_rows, a.batch, b, &s.k0, &s.kn);
+  return s;
+}
+// sequence and tile of a slot; `per` rows of an axis a row of the tensor, `tile` rows a tile
+__device__ __forceinline__ int slot_sequence(const int32_t* start, int64_t rows, int batch, int per, int tile, int slot, int* tile_index) {
+  int b = -1;
+  if (!start) {
+    // base(b) = b * each / tile + b is a known line: from a guess that is at most one too low
+    const int64_t each = rows / batch * per;
+    int64_t g = (int64_t)slot * tile / (each + tile);
+    while (g + 1 < batch && (g + 1) * each / tile + g + 1 <= slot) ++g;
+    b = (int)min(g, (int64_t)batch - 1);
+  } else {
+    // a wavefront looks at 64 sequences at a time: the last one whose first slot is not behind this one
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int at = 0; at < batch; at += kWave) {
+      const int i = at + lane;
+      const bool before = i < batch && start_of(start, rows, batch, min(i, batch)) * per / tile + i <= slot;
+      const unsigned long long m = __ballot(before);
+      if (!m) break;
+      b = at + 63 - __builtin_clzll(m);
+    }
+    b = max(b, 0);
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  const int64_t base = start_of(start, rows, batch, b) * per / tile + b;
+  *tile_index = __builtin_amdgcn_readfirstlane((int)(slot - base));
+  return b;
+}
+int64_t slots(int64_t rows, int batch, int per, int tile) { return rows * per / tile + batch; }
+
+// keys [lo, hi) that token i of a sequence sees
+__device__ __forceinline__ int key_end(const SeqAttn& a, const Seq& s, int i) { return a.causal ? min(max(i + s.kn - s.qn + 1, 0), s.kn) : s.kn; }
+__device__ __forceinline__ int key_begin(const SeqAttn& a, const Seq& s, int i) {
+  return a.window ? (int)max((int64_t)i + s.kn - s.qn - a.window + 1, (int64_t)0) : 0;
+}
+
+// ---- tiles on their way to LDS -----------------------------------------------
+// rows [j0, j0 + ROWS) of a matrix of n rows; rows behind it are zero
+template <class T, int D, int ROWS>
+struct Stage {
+  static constexpr int kPiece = 16 / sizeof(T), kRowPieces = D / kPiece, kAll = ROWS * kRowPieces, kN = (kAll + kThreads - 1) / kThreads;
+  static_assert(kAll % kThreads == 0 || kN == 1, "whole pieces a thread, or one for some");
+  u32x4_t v[kN];
+  __device__ __forceinline__ void load(const T* __restrict__ src, int64_t ld, int j0, int n) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int q = threadIdx.x + i * kThreads, row = min(j0 + q / kRowPieces, n - 1);
+      v[i] = *reinterpret_cast<const u32x4_t*>(src + row * ld + q % kRowPieces * kPiece);
+    }
+  }
+  __device__ __forceinline__ void store(T* dst, int j0, int n) const {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int q = threadIdx.x + i * kThreads, row = q / kRowPieces;
+      if (kAll % kThreads == 0 || q < kAll) *reinterpret_cast<u32x4_t*>(dst + row * kStride<T, D> + q % kRowPieces * kPiece) = j0 + row < n ? v[i] : u32x4_t{0u, 0u, 0u, 0u};
+    }
+  }
+};
+// the same where row r of the axis is (token r / group, head r % group)
+template <class T, int D, int ROWS>
+struct StageQ {
+  static constexpr int kPiece = 16 / sizeof(T), kRowPieces = D / kPiece, kAll = ROWS * kRowPieces, kN = (kAll + kThreads - 1) / kThreads;
+  static_assert(kAll % kThreads == 0 || kN == 1, "whole pieces a thread, or one for some");
+  u32x4_t v[kN];
+  __device__ __forceinline__ void load(const T* __restrict__ src, int64_t ld, int group, int r0, int n) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int q = threadIdx.x + i * kThreads, row = min(r0 + q / kRowPieces, n - 1), t = row / group;
+      v[i] = *reinterpret_cast<const u32x4_t*>(src + t * ld + (row - t * group) * D + q % kRowPieces * kPiece);
+    }
+  }
+  __device__ __forceinline__ void store(T* dst, int r0, int n) const {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int q = threadIdx.x + i * kThreads, row = q / kRowPieces;
+      if (kAll % kThreads == 0 || q < kAll) *reinterpret_cast<u32x4_t*>(dst + row * kStride<T, D> + q % kRowPieces * kPiece) = r0 + row < n ? v[i] : u32x4_t{0u, 0u, 0u, 0u};
+    }
+  }
+};
+
+// a lane's column of a transposed accumulator (32 values of d for each e) to memory as T or fp32
+template <class T, int D>
+__device__ __forceinline__ void store_column(T* p, const f32x16_t (&acc)[D / 32], float f, int half) {
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      T* to = p + 32 * e + 8 * i + 4 * half;
+      const float a = acc[e][4 * i] * f, b = acc[e][4 * i + 1] * f, c = acc[e][4 * i + 2] * f, d = acc[e][4 * i + 3] * f;
+      if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4_t*>(to) = bf16x4_t{static_cast<bf16_t>(a), static_cast<bf16_t>(b), static_cast<bf16_t>(c), static_cast<bf16_t>(d)};
+      else *reinterpret_cast<float4*>(to) = make_float4(a, b, c, d);
+    }
+}
+
+// ---- forward -----------------------------------------------------------------
+// rows of a block: 128, 32 a wavefront, keys in tiles of 64 (fp32: 32); or 32 that all wavefronts share, each with 32 of a tile's
+// 128 keys, for sequences with few queries: what a block then does is read keys, and it reads four times as many at a time
+template <class T, int RB>
+constexpr int kKeyTile = RB == 32 ? 128 : sizeof(T) == 2 ? 64 : 32;
+
+template <class T, int D, int RB>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_fwd_k(SeqAttn a) {
+  constexpr int KT = kKeyTile<T, RB>, NS = RB == 32 ? 1 : KT / 32, S = kStride<T, D>;
+  constexpr int kTileBytes = 2 * KT * S * (int)sizeof(T), kMergeBytes = RB == 32 ? 32 * D * 4 * (kWaves - 1) : 0;
+  __shared__ __attribute__((aligned(16))) char lds[kTileBytes > kMergeBytes ? kTileBytes : kMergeBytes];
+  __shared__ float merge_m[kWaves][32], merge_l[kWaves][32];
+  T* Ks = reinterpret_cast<T*>(lds);
+  T* Vs = Ks + KT * S;
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = a.hq / a.hk;
+  const int head = blockIdx.x % a.hk, split = blockIdx.y;
+  int tile;
+  // the last tiles see the most keys: they go first
+  const int slot = (int)(gridDim.x / a.hk - 1 - blockIdx.x / a.hk);
+  const int b = slot_sequence(a.q_start, a.q_rows, a.batch, group, RB, slot, &tile);
+  const Seq s = sequence(a, b);
+  const int rows = s.qn * group, r0 = tile * RB;
+  if (tile < 0 || r0 >= rows) return;
+
+  const int row = r0 + (RB == 32 ? 0 : 32 * wave) + col, rc = min(row, rows - 1), token = rc / group, h = head * group + rc - token * group;
+  const T* q = static_cast<const T*>(a.q) + (s.q0 + token) * a.ld_q + h * D + 8 * half;
+  Frag<T> qf[D / 16];
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) qf[kk] = load8(q + 16 * kk);
+  const int lo = key_begin(a, s, token), hi = row < rows ? key_end(a, s, token) : 0;
+  // of the wavefront's and of the block's rows: keys that any of them sees; all of the wavefront's see [w_lo, w_hi)
+  const int t_first = r0 / group, t_last = (min(r0 + RB, rows) - 1) / group;
+  int j_lo = key_begin(a, s, t_first), j_hi = key_end(a, s, t_last);
+  const int wr = r0 + (RB == 32 ? 0 : 32 * wave), wt0 = min(wr, rows - 1) / group, wt1 = (min(wr + 32, rows) - 1) / group;
+  const int w_lo = key_begin(a, s, wt1), w_hi = key_end(a, s, wt0), any_lo = key_begin(a, s, wt0), any_hi = wr < rows ? key_end(a, s, wt1) : 0;
+  if (a.splits > 1) {
+    const int n = j_hi > j_lo ? ((j_hi - j_lo + KT - 1) / KT + a.splits - 1) / a.splits * KT : 0;
+    j_lo = (int)min((int64_t)j_lo + (int64_t)split * n, (int64_t)j_hi);
+    j_hi = min(j_lo + n, j_hi);
+  }
+
+  const T* kp = static_cast<const T*>(a.k) + s.k0 * a.ld_k + head * D;
+  const T* vp = static_cast<const T*>(a.v) + s.k0 * a.ld_v + head * D;
+  f32x16_t o[D / 32];
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) o[e] = zero16();
+  float m = -INFINITY, l = 0.f;  // what exponentials are taken against (a score, without scale), this lane's part of their sum
+  const float c = a.scale * kLog2e;
+  Stage<T, D, KT> ks, vs;
+  if (j_lo < j_hi) {
+    ks.load(kp, a.ld_k, j_lo, s.kn);
+    vs.load(vp, a.ld_v, j_lo, s.kn);
+  }
+  for (int j0 = j_lo; j0 < j_hi; j0 += KT) {
+    ks.store(Ks, j0, s.kn);
+    vs.store(Vs, j0, s.kn);
+    __syncthreads();
+    if (j0 + KT < j_hi) {
+      ks.load(kp, a.ld_k, j0 + KT, s.kn);
+      vs.load(vp, a.ld_v, j0 + KT, s.kn);
+    }
+    const int base = RB == 32 ? 32 * wave : 0;
+    if (j0 + base < any_hi && j0 + base + 32 * NS > any_lo) {
+      f32x16_t p[NS];
+#pragma unroll
+      for (int t = 0; t < NS; ++t) p[t] = rows_times<T, D>(Ks, base + 32 * t, lane, qf);
+      // keys of this tile behind the split's last one belong to the next split: it starts at a tile, so none are
+      if (j0 + base < w_lo || j0 + base + 32 * NS > w_hi) {
+#pragma unroll
+        for (int t = 0; t < NS; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = j0 + base + 32 * t + row_of(r, half);
+            if (j < lo || j >= hi) p[t][r] = -INFINITY;
+          }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < NS; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, p[t][r]);
+      top = fmaxf(top, other_half(top));
+      // what exponentials are taken against follows the maximum only when it has risen by more than 2^8: until then they are
+      // at most 256 and nothing that 32 bits hold is lost, and the 64 products a tile of following it at once are saved
+      if (__any((top - m) * c > 8.f)) {
+        const float to = fmaxf(top, m), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - to) * c);
+        m = to;
+        l *= f;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[e][r] *= f;
+      }
+      const float mc = m == -INFINITY ? 0.f : m * c;
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < NS; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          p[t][r] = __builtin_amdgcn_exp2f(fmaf(p[t][r], c, -mc));
+          sum += p[t][r];
+        }
+      l += sum;
+#pragma unroll
+      for (int t = 0; t < NS; ++t) add_rows<T, D>(o, Vs, base + 32 * t, lane, p[t]);
+    }
+    __syncthreads();
+  }
+  l += other_half(l);
+
+  if constexpr (RB == 32) {  // the wavefronts' parts meet in the first one
+    if (lane < 32) {
+      merge_m[wave][lane] = m;
+      merge_l[wave][lane] = l;
+    }
+    float* x = reinterpret_cast<float*>(lds);
+    if (wave > 0) {
+      float* to = x + (wave - 1) * 32 * D + lane;
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) to[(e * 16 + r) * 64] = o[e][r];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    float top = m;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, merge_m[w][col]);
+    const float mm = top == -INFINITY ? 0.f : top;
+    float f = __builtin_amdgcn_exp2f((m - mm) * c);
+    l *= f;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[e][r] *= f;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) {
+      f = __builtin_amdgcn_exp2f((merge_m[w][col] - mm) * c);
+      l += merge_l[w][col] * f;
+      const float* from = x + (w - 1) * 32 * D + lane;
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[e][r] += from[(e * 16 + r) * 64] * f;
+    }
+    m = top;
+  }
+  if (row >= rows) return;
+  if (a.splits > 1) {
+    const int64_t at = ((int64_t)split * a.hq + h) * a.q_rows + s.q0 + token;
+    float* ml = a.part + (int64_t)a.splits * a.hq * a.q_rows * D;
+    store_column<float, D>(a.part + at * D, o, 1.f, half);
+    if (half == 0) {
+      ml[2 * at] = m;
+      ml[2 * at + 1] = l;
+    }
+    return;
+  }
+  store_column<T, D>(static_cast<T*>(a.out) + (s.q0 + token) * a.ld_o + h * D, o, l == 0.f ? 0.f : 1.f / l, half);
+  if (half == 0) a.lse[(int64_t)h * a.q_rows + s.q0 + token] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
+}
+
+// joins the parts of a row whose keys were shared out: a wavefront a (token, head)
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void seq_join_k(SeqAttn a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = a.hq / a.hk, head = blockIdx.x % a.hk;
+  constexpr int RB = 32;
+  int tile;
+  const int b = slot_sequence(a.q_start, a.q_rows, a.batch, group, RB, (int)(blockIdx.x / a.hk), &tile);
+  const Seq s = sequence(a, b);
+  const int rows = s.qn * group;
+  if (tile < 0) return;
+  const float* ml = a.part + (int64_t)a.splits * a.hq * a.q_rows * D;
+  const int64_t step = (int64_t)a.hq * a.q_rows;
+  const float c = a.scale * kLog2e;
+  for (int row = tile * RB + wave; row < min(rows, (tile + 1) * RB); row += kWaves) {
+    const int token = row / group, h = head * group + row - token * group;
+    const int64_t at = (int64_t)h * a.q_rows + s.q0 + token;
+    float m = -INFINITY;
+    for (int i = 0; i < a.splits; ++i) m = fmaxf(m, ml[2 * (at + i * step)]);
+    const float mm = m == -INFINITY ? 0.f : m;
+    float l = 0.f, o[D / 64 > 0 ? D / 64 : 1] = {};
+    for (int i = 0; i < a.splits; ++i) {
+      const int64_t p = at + i * step;
+      const float part = ml[2 * p + 1], f = __builtin_amdgcn_exp2f((ml[2 * p] - mm) * c);
+      if (part == 0.f) continue;  // no key of its own
+      l += part * f;
+#pragma unroll
+      for (int e = 0; e < (D + 63) / 64; ++e)
+        if (lane + 64 * e < D) o[e] += a.part[p * D + lane + 64 * e] * f;
+    }
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    T* out = static_cast<T*>(a.out) + (s.q0 + token) * a.ld_o + h * D;
+#pragma unroll
+    for (int e = 0; e < (D + 63) / 64; ++e)
+      if (lane + 64 * e < D) out[lane + 64 * e] = static_cast<T>(o[e] * f);
+    if (lane == 0) a.lse[at] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
+  }
+}
+
+// ---- backward ----------------------------------------------------------------
+// gradient of the queries: 32 rows a wavefront, keys in tiles.  Also leaves delta = out . d_out of each row, formed by the matrix
+// instructions that form d_out . v, so that the two agree to the bit where a query sees one key and its gradient is zero.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_bwd_q_k(SeqAttn a) {
+  constexpr int RB = 128, KT = kKeyTile<T, RB>, S = kStride<T, D>;
+  __shared__ __attribute__((aligned(16))) T Ks[KT * S];
+  __shared__ __attribute__((aligned(16))) T Vs[KT * S];
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = a.hq / a.hk, head = blockIdx.x % a.hk;
+  int tile;
+  const int slot = (int)(gridDim.x / a.hk - 1 - blockIdx.x / a.hk);
+  const int b = slot_sequence(a.q_start, a.q_rows, a.batch, group, RB, slot, &tile);
+  const Seq s = sequence(a, b);
+  const int rows = s.qn * group, r0 = tile * RB;
+  if (tile < 0 || r0 >= rows) return;
+
+  const int row = r0 + 32 * wave + col, rc = min(row, rows - 1), token = rc / group, h = head * group + rc - token * group;
+  const T* q = static_cast<const T*>(a.q) + (s.q0 + token) * a.ld_q + h * D + 8 * half;
+  const int64_t o_at = (s.q0 + token) * a.ld_o + h * D + 8 * half, stat = (int64_t)h * a.q_rows + s.q0 + token;
+  Frag<T> qf[D / 16], df[D / 16];
+  f32x16_t oo = zero16();
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) {
+    qf[kk] = load8(q + 16 * kk);
+    df[kk] = load8(static_cast<const T*>(a.dout) + o_at + 16 * kk);
+    oo = mma(load8(static_cast<const T*>(a.out) + o_at + 16 * kk), df[kk], oo);  // [row of out][row of d_out]
+  }
+  float delta = 0.f;  // the diagonal: row col, in the half that holds it
+#pragma unroll
+  for (int r = 0; r < 16; ++r) delta = row_of(r, half) == col ? oo[r] : delta;
+  {
+    const float other = other_half(delta);
+    if (((col >> 2) & 1) != half) delta = other;
+  }
+  const float lse2 = a.lse[stat] * kLog2e;
+  if (row < rows && half == 0) a.delta[stat] = delta;
+  const int lo = key_begin(a, s, token), hi = row < rows ? key_end(a, s, token) : 0;
+  const int t_first = r0 / group, t_last = (min(r0 + RB, rows) - 1) / group;
+  const int j_lo = key_begin(a, s, t_first), j_hi = key_end(a, s, t_last);
+  const int wr = r0 + 32 * wave, wt0 = min(wr, rows - 1) / group, wt1 = (min(wr + 32, rows) - 1) / group;
+  const int w_lo = key_begin(a, s, wt1), w_hi = key_end(a, s, wt0), any_lo = key_begin(a, s, wt0), any_hi = wr < rows ? key_end(a, s, wt1) : 0;
+
+  const T* kp = static_cast<const T*>(a.k) + s.k0 * a.ld_k + head * D;
+  const T* vp = static_cast<const T*>(a.v) + s.k0 * a.ld_v + head * D;
+  f32x16_t dq[D / 32];
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) dq[e] = zero16();
+  const float c = a.scale * kLog2e;
+  Stage<T, D, KT> ks, vs;
+  if (j_lo < j_hi) {
+    ks.load(kp, a.ld_k, j_lo, s.kn);
+    vs.load(vp, a.ld_v, j_lo, s.kn);
+  }
+  for (int j0 = j_lo; j0 < j_hi; j0 += KT) {
+    ks.store(Ks, j0, s.kn);
+    vs.store(Vs, j0, s.kn);
+    __syncthreads();
+    if (j0 + KT < j_hi) {
+      ks.load(kp, a.ld_k, j0 + KT, s.kn);
+      vs.load(vp, a.ld_v, j0 + KT, s.kn);
+    }
+#pragma unroll
+    for (int t = 0; t < KT / 32; ++t) {
+      const int j = j0 + 32 * t;
+      if (j >= any_hi || j + 32 <= any_lo) continue;
+      f32x16_t p = rows_times<T, D>(Ks, 32 * t, lane, qf);
+      f32x16_t dp = rows_times<T, D>(Vs, 32 * t, lane, df);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, -lse2)) * (dp[r] - delta);
+      if (j < w_lo || j + 32 > w_hi) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = j + row_of(r, half);
+          if (key < lo || key >= hi) dp[r] = 0.f;
+        }
+      }
+      add_rows<T, D>(dq, Ks, 32 * t, lane, dp);
+    }
+    __syncthreads();
+  }
+  if (row < rows) store_column<T, D>(static_cast<T*>(a.dq) + (s.q0 + token) * a.ld_q + h * D, dq, a.scale, half);
+}
+
+// gradients of keys and values: 32 keys a wavefront, the queries of all heads of the group in tiles of 32 rows
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 2 : 1) void seq_bwd_k_k(SeqAttn a) {
+  constexpr int RB = 128, QT = 32, S = kStride<T, D>;
+  __shared__ __attribute__((aligned(16))) T Qs[QT * S];
+  __shared__ __attribute__((aligned(16))) T Cs[QT * S];
+  __shared__ __attribute__((aligned(16))) float stats[2][QT];
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = a.hq / a.hk, head = blockIdx.x % a.hk;
+  int tile;
+  const int slot = (int)(blockIdx.x / a.hk);  // the first keys are seen by the most queries
+  const int b = slot_sequence(a.k_start, a.k_rows, a.batch, 1, RB, slot, &tile);
+  const Seq s = sequence(a, b);
+  const int j0 = tile * RB;
+  if (tile < 0 || j0 >= s.kn) return;
+
+  const int key = j0 + 32 * wave + col, kc = min(key, s.kn - 1);
+  const T* kp = static_cast<const T*>(a.k) + (s.k0 + kc) * a.ld_k + head * D + 8 * half;
+  const T* vp = static_cast<const T*>(a.v) + (s.k0 + kc) * a.ld_v + head * D + 8 * half;
+  Frag<T> kf[D / 16], vf[D / 16];
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) {
+    kf[kk] = load8(kp + 16 * kk);
+    vf[kk] = load8(vp + 16 * kk);
+  }
+  const int rows = s.qn * group, off = s.kn - s.qn;
+  // rows [lo, hi) whose queries see key j: token + off >= j, token + off - window < j
+  const auto row_begin = [&](int j) { return a.causal ? (int)min((int64_t)max(j - off, 0) * group, (int64_t)rows) : 0; };
+  const auto row_end = [&](int j) { return a.window ? (int)min(max((int64_t)j - off + a.window, (int64_t)0) * group, (int64_t)rows) : rows; };
+  const int lo = row_begin(kc), hi = key < s.kn ? row_end(kc) : 0;
+  const int k_last = min(j0 + RB, s.kn) - 1;
+  const int r_lo = row_begin(j0), r_hi = row_end(k_last);
+  const int wk0 = min(j0 + 32 * wave, s.kn - 1), wk1 = min(j0 + 32 * wave + 31, s.kn - 1);
+  const bool wave_on = j0 + 32 * wave < s.kn, wave_whole = j0 + 32 * wave + 32 <= s.kn;
+  const int any_lo = row_begin(wk0), any_hi = wave_on ? row_end(wk1) : 0, w_lo = row_begin(wk1), w_hi = wave_whole ? row_end(wk0) : 0;
+
+  const T* qp = static_cast<const T*>(a.q) + s.q0 * a.ld_q + head * group * D;
+  const T* cp = static_cast<const T*>(a.dout) + s.q0 * a.ld_o + head * group * D;
+  f32x16_t dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) {
+    dk[e] = zero16();
+    dv[e] = zero16();
+  }
+  const float c = a.scale * kLog2e;
+  StageQ<T, D, QT> qs, cs;
+  float stat = 0.f;
+  const auto load = [&](int r) {
+    qs.load(qp, a.ld_q, group, r, rows);
+    cs.load(cp, a.ld_o, group, r, rows);
+    if (threadIdx.x < 2 * QT) {
+      const int at = min(r + ((int)threadIdx.x & (QT - 1)), rows - 1), t = at / group;
+      const int64_t i = (int64_t)(head * group + at - t * group) * a.q_rows + s.q0 + t;
+      stat = (int)threadIdx.x < QT ? a.lse[i] * kLog2e : a.delta[i];
+    }
+  };
+  if (r_lo < r_hi) load(r_lo);
+  for (int r = r_lo; r < r_hi; r += QT) {
+    qs.store(Qs, r, rows);
+    cs.store(Cs, r, rows);
+    if (threadIdx.x < 2 * QT) stats[threadIdx.x / QT][threadIdx.x & (QT - 1)] = stat;
+    __syncthreads();
+    if (r + QT < r_hi) load(r + QT);
+    if (r < any_hi && r + QT > any_lo) {
+      f32x16_t p = rows_times<T, D>(Qs, 0, lane, kf);
+      f32x16_t dp = rows_times<T, D>(Cs, 0, lane, vf);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 ls = *reinterpret_cast<const float4*>(&stats[0][8 * i + 4 * half]), de = *reinterpret_cast<const float4*>(&stats[1][8 * i + 4 * half]);
+        const float lsv[4] = {ls.x, ls.y, ls.z, ls.w}, dev[4] = {de.x, de.y, de.z, de.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          p[4 * i + j] = __builtin_amdgcn_exp2f(fmaf(p[4 * i + j], c, -lsv[j]));
+          dp[4 * i + j] = p[4 * i + j] * (dp[4 * i + j] - dev[j]);
+        }
+      }
+      if (r < w_lo || r + QT > w_hi) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int at = r + row_of(i, half);
+          if (at < lo || at >= hi) {
+            p[i] = 0.f;
+            dp[i] = 0.f;
+          }
+        }
+      }
+      add_rows<T, D>(dv, Cs, 0, lane, p);
+      add_rows<T, D>(dk, Qs, 0, lane, dp);
+    }
+    __syncthreads();
+  }
+  if (key < s.kn) {
+    store_column<T, D>(static_cast<T*>(a.dk) + (s.k0 + key) * a.ld_k + head * D, dk, a.scale, half);
+    store_column<T, D>(static_cast<T*>(a.dv) + (s.k0 + key) * a.ld_v + head * D, dv, 1.f, half);
+  }
+}
+
+// ---- launches ----------------------------------------------------------------
+// few queries a sequence, on the average (their number is not known on the host): blocks of 32 rows
+bool few_rows(const SeqAttn& a) { return a.q_rows * (a.hq / a.hk) <= (int64_t)32 * a.batch; }
+// keys are shared out among blocks while there are fewer than four blocks a compute unit, each keeping two tiles
+int splits(const SeqAttn& a) {
+  if (!few_rows(a) || a.q_rows == 0) return 1;
+  const int64_t blocks = slots(a.q_rows, a.batch, a.hq / a.hk, 32) * a.hk, keys = (a.k_rows + a.batch - 1) / a.batch;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({1024 / blocks, keys / 256, 32}));
+}
+
+template <class T, int D>
+void forward(const SeqAttn& a, hipStream_t st) {
+  const int group = a.hq / a.hk;
+  if (few_rows(a)) {
+    const unsigned n = (unsigned)(slots(a.q_rows, a.batch, group, 32) * a.hk);
+    seq_fwd_k<T, D, 32><<<dim3(n, (unsigned)a.splits), kThreads, 0, st>>>(a);
+    if (a.splits > 1) seq_join_k<T, D><<<n, kThreads, 0, st>>>(a);
+  } else {
+    seq_fwd_k<T, D, 128><<<(unsigned)(slots(a.q_rows, a.batch, group, 128) * a.hk), kThreads, 0, st>>>(a);
+  }
+}
+template <class T, int D>
+void backward(const SeqAttn& a, hipStream_t st) {
+  if (a.q_rows) seq_bwd_q_k<T, D><<<(unsigned)(slots(a.q_rows, a.batch, a.hq / a.hk, 128) * a.hk), kThreads, 0, st>>>(a);
+  if (a.k_rows) seq_bwd_k_k<T, D><<<(unsigned)(slots(a.k_rows, a.batch, 1, 128) * a.hk), kThreads, 0, st>>>(a);
+}
+
+#define MREM_SEQ_DISPATCH(f)                                    \
+  do {                                                          \
+    if (a.dt == DT_BF16) {                                      \
+      if (a.d == 32) f<bf16_t, 32>(a, st);                      \
+      else if (a.d == 64) f<bf16_t, 64>(a, st);                 \
+      else f<bf16_t, 128>(a, st);                               \
+    } else {                                                    \
+      if (a.d == 32) f<float, 32>(a, st);                       \
+      else if (a.d == 64) f<float, 64>(a, st);                  \
+      else f<float, 128>(a, st);                                \
+    }                                                           \
+  } while (0)
+
+}  // namespace
+
+size_t seq_attn_fwd_bytes(const SeqAttn& a) {
+  const int n = splits(a);
+  return n > 1 ? (size_t)n * a.hq * a.q_rows * (a.d + 2) * 4 : 0;
+}
+size_t seq_attn_bwd_bytes(const SeqAttn& a) { return (size_t)a.hq * a.q_rows * 4; }
+
+void seq_attn_fwd(SeqAttn a, void* workspace, hipStream_t st) {
+  a.splits = splits(a);
+  a.part = static_cast<float*>(workspace);
+  MREM_SEQ_DISPATCH(forward);
+}
+void seq_attn_bwd(SeqAttn a, void* workspace, hipStream_t st) {
+  a.delta = static_cast<float*>(workspace);
+  MREM_SEQ_DISPATCH(backward);
+}
+
+}  // namespace mrem
