@@ -383,7 +383,7 @@ mrem_status mrem_attention_backward(const mrem_attention_config* cfg, const void
  *   loss_out      device fp32 [1] or NULL (out)
  *   grad          device dtype [rows, vocab], rows ld_grad elements apart, or NULL (out): of loss with respect to logits; may be
  *                 logits themselves (ld_grad = ld), and may not overlap them otherwise
- * vocab 1..2^20, k 1..1024, temperature > 0, strides >= vocab.  Pointers need the alignment of their elements only.  rows = 0
+ * vocab 1..2^19, k 1..1024, temperature > 0, strides >= vocab.  Pointers need the alignment of their elements only.  rows = 0
  * sets loss_out to 0; rows < 2^22.
  */
 mrem_status mrem_distill_loss(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const float* top_logits,

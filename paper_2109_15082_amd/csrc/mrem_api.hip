@@ -1575,7 +1575,7 @@ extern "C" mrem_status mrem_distill_loss(const void* logits, int32_t dtype, int6
   const auto bad = [](mrem_status st, const char* what) { return fail(nullptr, st, std::string("mrem_distill_loss: ") + what); };
   if (!known_dtype(dtype)) return bad(MREM_EINVAL, "dtype must be MREM_BF16 or MREM_FP32");
   if (rows < 0 || rows >= (int64_t)1 << 22) return bad(MREM_ESHAPE, "rows must be in 0..2^22-1");  // a block of up to 1024 threads each
-  if (vocab < 1 || vocab > kDistillMaxVocab) return bad(MREM_ESHAPE, "vocab must be in 1..2^20");
+  if (vocab < 1 || vocab > kDistillMaxVocab) return bad(MREM_ESHAPE, "vocab must be in 1..2^19");
   if (k < 1 || k > kDistillMaxK) return bad(MREM_ESHAPE, "k must be in 1..1024");
   if (ld < vocab || (grad && ld_grad < vocab)) return bad(MREM_ESHAPE, "rows overlap: stride below vocab");
   if (!(temperature > 0.f) || !std::isfinite(temperature)) return bad(MREM_EINVAL, "temperature must be positive");

@@ -340,7 +340,7 @@ void seq_attn_fwd(SeqAttn a, void* workspace, hipStream_t st);
 void seq_attn_bwd(SeqAttn a, void* workspace, hipStream_t st);
 
 constexpr int kDistillMaxK = 1024;
-constexpr int kDistillMaxVocab = 1 << 20;
+constexpr int kDistillMaxVocab = 1 << 19;
 struct DistillArg {
   const void* x;
   void* grad;

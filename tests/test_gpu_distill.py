@@ -104,7 +104,7 @@ def test_loss_and_gradient(env, rows, vocab, k, tail, dtype):
 
 def test_the_largest_vocabulary(env):
     torch, B = env
-    s = inputs(torch, 1, 1 << 20, 1024, "float32", 1)
+    s = inputs(torch, 1, 1 << 19, 1024, "float32", 1)
     check(torch, s, run(torch, B, s))
 
 

@@ -95,7 +95,7 @@ def test_distill_refusals(B):
     good = dict(x=FAKE, dtype=0, rows=4, vocab=100, ld=100, top=FAKE, index=FAKE, k=8, tlse=None, temp=1.0, w=None, scale=1.0, lr=FAKE, lo=FAKE, g=None, ldg=100)
     odd = ctypes.c_void_p(0x1001)
     bad = [(dict(x=None), "logits"), (dict(x=odd), "logits"), (dict(dtype=5), "dtype"), (dict(rows=-1), "rows"), (dict(rows=1 << 22), "rows"), (dict(vocab=0), "vocab"),
-           (dict(vocab=(1 << 20) + 1, ld=1 << 21), "vocab"), (dict(ld=99), "stride"), (dict(g=FAKE, ldg=99), "stride"), (dict(k=0), "k must"), (dict(k=1025), "k must"),
+           (dict(vocab=(1 << 19) + 1, ld=1 << 20), "vocab"), (dict(ld=99), "stride"), (dict(g=FAKE, ldg=99), "stride"), (dict(k=0), "k must"), (dict(k=1025), "k must"),
            (dict(temp=0.0), "temperature"), (dict(temp=-1.0), "temperature"), (dict(temp=math.nan), "temperature"), (dict(scale=math.inf), "scale"), (dict(top=None), "top_logits"),
            (dict(index=None), "top_index"), (dict(lr=None), "loss_rows"), (dict(lr=odd), "misaligned"), (dict(tlse=odd), "misaligned"), (dict(g=odd), "misaligned"),
            (dict(g=FAKE, ldg=104), "in place")]
