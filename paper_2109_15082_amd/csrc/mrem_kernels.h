@@ -329,7 +329,8 @@ struct SeqAttn {
   int64_t q_rows, k_rows, ld_q, ld_k, ld_v, ld_o;
   const void *q, *k, *v, *dout;
   void *out, *dq, *dk, *dv;
-  float *lse, *delta;  // [hq, q_rows]
+  float* lse;    // [hq, q_rows]
+  float* delta;  // [hk, q_rows, hq / hk] pairs: lse times log2(e), out . d_out
   const int32_t *q_start, *k_start, *q_len, *k_len;
   float* part;  // partial results of keys shared out among blocks
   int splits;

@@ -212,24 +212,48 @@ struct Stage {
     }
   }
 };
-// the same where row r of the axis is (token r / group, head r % group)
-template <class T, int D, int ROWS>
-struct StageQ {
-  static constexpr int kPiece = 16 / sizeof(T), kRowPieces = D / kPiece, kAll = ROWS * kRowPieces, kN = (kAll + kThreads - 1) / kThreads;
-  static_assert(kAll % kThreads == 0 || kN == 1, "whole pieces a thread, or one for some");
-  u32x4_t v[kN];
-  __device__ __forceinline__ void load(const T* __restrict__ src, int64_t ld, int group, int r0, int n) {
+// Rows of the packed axis, (token r / group, head r % group), tile after tile: a thread's rows are kThreads / pieces apart and move on
+// by a tile's rows, so their places advance by a quotient and a remainder that are divided once.
+template <class T, int D, int ROWS, int THREADS>
+struct QueryRows {
+  static constexpr int kPiece = 16 / sizeof(T), kRowPieces = D / kPiece, kN = ROWS * kRowPieces / THREADS, kApart = THREADS / kRowPieces;
+  static_assert(ROWS * kRowPieces % THREADS == 0, "whole pieces a thread");
+  int token[kN];
+  int head[kN];
+  u32x4_t q[kN], c[kN];
+  __device__ __forceinline__ void start(int group, int r0) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int q = threadIdx.x + i * kThreads, row = min(r0 + q / kRowPieces, n - 1), t = row / group;
-      v[i] = *reinterpret_cast<const u32x4_t*>(src + t * ld + (row - t * group) * D + q % kRowPieces * kPiece);
+      const int row = r0 + threadIdx.x / kRowPieces + i * kApart, t = row / group;
+      token[i] = t;
+      head[i] = row - t * group;
     }
   }
-  __device__ __forceinline__ void store(T* dst, int r0, int n) const {
+  // rows r0 + ... of the two tensors (zeros behind n); then the next tile's places
+  __device__ __forceinline__ void load(const T* __restrict__ qs, int64_t ld_q, const T* __restrict__ cs, int64_t ld_c, int r0, int n, int group, int quotient, int rest) {
+    const int at = threadIdx.x % kRowPieces * kPiece;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int q = threadIdx.x + i * kThreads, row = q / kRowPieces;
-      if (kAll % kThreads == 0 || q < kAll) *reinterpret_cast<u32x4_t*>(dst + row * kStride<T, D> + q % kRowPieces * kPiece) = r0 + row < n ? v[i] : u32x4_t{0u, 0u, 0u, 0u};
+      q[i] = c[i] = u32x4_t{0u, 0u, 0u, 0u};
+      if (r0 + (int)(threadIdx.x / kRowPieces) + i * kApart < n) {
+        const int col = head[i] * D + at;
+        q[i] = *reinterpret_cast<const u32x4_t*>(qs + (int64_t)token[i] * ld_q + col);
+        c[i] = *reinterpret_cast<const u32x4_t*>(cs + (int64_t)token[i] * ld_c + col);
+      }
+      head[i] += rest;
+      token[i] += quotient;
+      if (head[i] >= group) {
+        head[i] -= group;
+        token[i] += 1;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* qs, T* cs) const {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int to = (threadIdx.x / kRowPieces + i * kApart) * kStride<T, D> + threadIdx.x % kRowPieces * kPiece;
+      *reinterpret_cast<u32x4_t*>(qs + to) = q[i];
+      *reinterpret_cast<u32x4_t*>(cs + to) = c[i];
     }
   }
 };
@@ -485,7 +509,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_bwd_q_k(
     if (((col >> 2) & 1) != half) delta = other;
   }
   const float lse2 = a.lse[stat] * kLog2e;
-  if (row < rows && half == 0) a.delta[stat] = delta;
+  if (row < rows && half == 0) reinterpret_cast<float2*>(a.delta)[((int64_t)head * a.q_rows + s.q0) * group + row] = make_float2(lse2, delta);
   const int lo = key_begin(a, s, token), hi = row < rows ? key_end(a, s, token) : 0;
   const int t_first = r0 / group, t_last = (min(r0 + RB, rows) - 1) / group;
   const int j_lo = key_begin(a, s, t_first), j_hi = key_end(a, s, t_last);
@@ -533,14 +557,33 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_bwd_q_k(
   if (row < rows) store_column<T, D>(static_cast<T*>(a.dq) + (s.q0 + token) * a.ld_q + h * D, dq, a.scale, half);
 }
 
-// gradients of keys and values: 32 keys a wavefront, the queries of all heads of the group in tiles of 32 rows
+// Gradients of keys and values: 128 keys a block, 32 a wavefront, the queries of all heads of the group in tiles that the wavefronts
+// share.  Both gradients, both operands and two tiles of scores are some 230 registers a lane at head dimension 128, which allows two
+// wavefronts a SIMD.  They are two that own the same keys and take every other tile of rows, and meet in LDS at the end: with
+// other keys for the second one there would be half as many blocks, each twice as long, and under a causal mask the block of the
+// first keys would outlast the others by half of the kernel's time (2 x 4096 tokens, 32 heads on 8: 1230 us).
+// Tiles are written to LDS one step ahead, so that there is one barrier a step.  (fp32 fills the registers with one wavefront.)
+template <class T>
+constexpr int kRowParts = sizeof(T) == 2 ? 2 : 1;
+// fragments of the values (of D / 16) that lie in LDS, a thread's own, since the registers do not hold them
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 2 : 1) void seq_bwd_k_k(SeqAttn a) {
-  constexpr int RB = 128, QT = 32, S = kStride<T, D>;
-  __shared__ __attribute__((aligned(16))) T Qs[QT * S];
-  __shared__ __attribute__((aligned(16))) T Cs[QT * S];
-  __shared__ __attribute__((aligned(16))) float stats[2][QT];
-  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+constexpr int kValuesInLds = sizeof(T) == 2 && D == 128 ? 8 : 0;
+// rows of a wavefront's tile
+template <class T, int D>
+constexpr int kQueryTile = sizeof(T) == 2 && D == 32 ? 64 : 32;
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads* kRowParts<T>, kRowParts<T>) void seq_bwd_k_k(SeqAttn a) {
+  constexpr int P = kRowParts<T>, NT = kThreads * P, RB = 128, WT = kQueryTile<T, D>, QT = WT * P, S = kStride<T, D>;
+  constexpr int kTileBytes = 4 * QT * S * (int)sizeof(T), kMergeBytes = P > 1 ? RB * D * 4 : 0;
+  __shared__ __attribute__((aligned(16))) char tiles[kTileBytes > kMergeBytes ? kTileBytes : kMergeBytes];
+  const auto Qs = [&](int buf) { return reinterpret_cast<T*>(tiles) + buf * QT * S; };
+  const auto Cs = [&](int buf) { return reinterpret_cast<T*>(tiles) + (2 + buf) * QT * S; };
+  constexpr int VL = kValuesInLds<T, D>, VR = D / 16 - VL;
+  __shared__ Frag<T> v_lds[VL > 0 ? VL : 1][VL > 0 ? NT : 1];
+  __shared__ __attribute__((aligned(16))) float stats[2][2][QT];  // log-sum-exp times log2(e), delta
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = w % kWaves, part = w / kWaves;
   const int group = a.hq / a.hk, head = blockIdx.x % a.hk;
   int tile;
   const int slot = (int)(blockIdx.x / a.hk);  // the first keys are seen by the most queries
@@ -552,11 +595,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 2 : 1) void s
   const int key = j0 + 32 * wave + col, kc = min(key, s.kn - 1);
   const T* kp = static_cast<const T*>(a.k) + (s.k0 + kc) * a.ld_k + head * D + 8 * half;
   const T* vp = static_cast<const T*>(a.v) + (s.k0 + kc) * a.ld_v + head * D + 8 * half;
-  Frag<T> kf[D / 16], vf[D / 16];
+  Frag<T> kf[D / 16], vf[VR > 0 ? VR : 1];
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) {
     kf[kk] = load8(kp + 16 * kk);
-    vf[kk] = load8(vp + 16 * kk);
+    if (kk < VR) vf[kk] = load8(vp + 16 * kk);
+    else v_lds[kk - VR][threadIdx.x] = load8(vp + 16 * kk);
   }
   const int rows = s.qn * group, off = s.kn - s.qn;
   // rows [lo, hi) whose queries see key j: token + off >= j, token + off - window < j
@@ -571,6 +615,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 2 : 1) void s
 
   const T* qp = static_cast<const T*>(a.q) + s.q0 * a.ld_q + head * group * D;
   const T* cp = static_cast<const T*>(a.dout) + s.q0 * a.ld_o + head * group * D;
+  const float2* sp = reinterpret_cast<const float2*>(a.delta) + ((int64_t)head * a.q_rows + s.q0) * group;
   f32x16_t dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) {
@@ -578,30 +623,49 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 2 : 1) void s
     dv[e] = zero16();
   }
   const float c = a.scale * kLog2e;
-  StageQ<T, D, QT> qs, cs;
-  float stat = 0.f;
+  const int quotient = QT / group, rest = QT - quotient * group;
+  QueryRows<T, D, QT, NT> qr;
+  float2 stat = make_float2(0.f, 0.f);
   const auto load = [&](int r) {
-    qs.load(qp, a.ld_q, group, r, rows);
-    cs.load(cp, a.ld_o, group, r, rows);
-    if (threadIdx.x < 2 * QT) {
-      const int at = min(r + ((int)threadIdx.x & (QT - 1)), rows - 1), t = at / group;
-      const int64_t i = (int64_t)(head * group + at - t * group) * a.q_rows + s.q0 + t;
-      stat = (int)threadIdx.x < QT ? a.lse[i] * kLog2e : a.delta[i];
+    qr.load(qp, a.ld_q, cp, a.ld_o, r, rows, group, quotient, rest);
+    if ((int)threadIdx.x < QT) stat = sp[min(r + (int)threadIdx.x, rows - 1)];
+  };
+  const auto store = [&](int buf) {
+    qr.store(Qs(buf), Cs(buf));
+    if ((int)threadIdx.x < QT) {
+      stats[buf][0][threadIdx.x] = stat.x;
+      stats[buf][1][threadIdx.x] = stat.y;
     }
   };
-  if (r_lo < r_hi) load(r_lo);
-  for (int r = r_lo; r < r_hi; r += QT) {
-    qs.store(Qs, r, rows);
-    cs.store(Cs, r, rows);
-    if (threadIdx.x < 2 * QT) stats[threadIdx.x / QT][threadIdx.x & (QT - 1)] = stat;
+  if (r_lo < r_hi) {
+    qr.start(group, r_lo);
+    load(r_lo);
+    store(0);
+    if (r_lo + QT < r_hi) load(r_lo + QT);
     __syncthreads();
-    if (r + QT < r_hi) load(r + QT);
-    if (r < any_hi && r + QT > any_lo) {
-      f32x16_t p = rows_times<T, D>(Qs, 0, lane, kf);
-      f32x16_t dp = rows_times<T, D>(Cs, 0, lane, vf);
+  }
+  for (int r = r_lo, buf = 0; r < r_hi; r += QT, buf ^= 1) {
+    if (r + QT < r_hi) {
+      store(buf ^ 1);
+      if (r + 2 * QT < r_hi) load(r + 2 * QT);
+    }
+#pragma unroll
+    for (int t = 0; t < WT / 32; ++t) {
+      const int at_t = part * WT + 32 * t, rt = r + at_t;
+      if (rt >= any_hi || rt + 32 <= any_lo) continue;
+      f32x16_t p = rows_times<T, D>(Qs(buf), at_t, lane, kf);
+      f32x16_t dp = zero16();
+      {
+        const T* cr = Cs(buf) + (at_t + col) * S + 8 * half;
+#pragma unroll
+        for (int kk = 0; kk < VR; ++kk) dp = mma(load8(cr + 16 * kk), vf[kk], dp);
+#pragma unroll
+        for (int kk = VR; kk < D / 16; ++kk) dp = mma(load8(cr + 16 * kk), v_lds[kk - VR][threadIdx.x], dp);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float4 ls = *reinterpret_cast<const float4*>(&stats[0][8 * i + 4 * half]), de = *reinterpret_cast<const float4*>(&stats[1][8 * i + 4 * half]);
+        const float4 ls = *reinterpret_cast<const float4*>(&stats[buf][0][at_t + 8 * i + 4 * half]);
+        const float4 de = *reinterpret_cast<const float4*>(&stats[buf][1][at_t + 8 * i + 4 * half]);
         const float lsv[4] = {ls.x, ls.y, ls.z, ls.w}, dev[4] = {de.x, de.y, de.z, de.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -609,20 +673,42 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 2 : 1) void s
           dp[4 * i + j] = p[4 * i + j] * (dp[4 * i + j] - dev[j]);
         }
       }
-      if (r < w_lo || r + QT > w_hi) {
+      if (rt < w_lo || rt + 32 > w_hi) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int at = r + row_of(i, half);
+          const int at = rt + row_of(i, half);
           if (at < lo || at >= hi) {
             p[i] = 0.f;
             dp[i] = 0.f;
           }
         }
       }
-      add_rows<T, D>(dv, Cs, 0, lane, p);
-      add_rows<T, D>(dk, Qs, 0, lane, dp);
+      add_rows<T, D>(dv, Cs(buf), at_t, lane, p);
+      add_rows<T, D>(dk, Qs(buf), at_t, lane, dp);
     }
     __syncthreads();
+  }
+  if constexpr (P > 1) {  // the second part's sums are added to the first's, one gradient after the other
+    float* x = reinterpret_cast<float*>(tiles) + wave * 32 * D + lane;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      f32x16_t(&acc)[D / 32] = g ? dv : dk;
+      if (part > 0) {
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[(e * 16 + i) * 64] = acc[e][i];
+      }
+      __syncthreads();
+      if (part == 0) {
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[e][i] += x[(e * 16 + i) * 64];
+      }
+      if (g == 0) __syncthreads();
+    }
+    if (part > 0) return;
   }
   if (key < s.kn) {
     store_column<T, D>(static_cast<T*>(a.dk) + (s.k0 + key) * a.ld_k + head * D, dk, a.scale, half);
@@ -654,7 +740,7 @@ void forward(const SeqAttn& a, hipStream_t st) {
 template <class T, int D>
 void backward(const SeqAttn& a, hipStream_t st) {
   if (a.q_rows) seq_bwd_q_k<T, D><<<(unsigned)(slots(a.q_rows, a.batch, a.hq / a.hk, 128) * a.hk), kThreads, 0, st>>>(a);
-  if (a.k_rows) seq_bwd_k_k<T, D><<<(unsigned)(slots(a.k_rows, a.batch, 1, 128) * a.hk), kThreads, 0, st>>>(a);
+  if (a.k_rows) seq_bwd_k_k<T, D><<<(unsigned)(slots(a.k_rows, a.batch, 1, 128) * a.hk), kThreads * kRowParts<T>, 0, st>>>(a);
 }
 
 #define MREM_SEQ_DISPATCH(f)                                    \
@@ -676,7 +762,7 @@ size_t seq_attn_fwd_bytes(const SeqAttn& a) {
   const int n = splits(a);
   return n > 1 ? (size_t)n * a.hq * a.q_rows * (a.d + 2) * 4 : 0;
 }
-size_t seq_attn_bwd_bytes(const SeqAttn& a) { return (size_t)a.hq * a.q_rows * 4; }
+size_t seq_attn_bwd_bytes(const SeqAttn& a) { return (size_t)a.hq * a.q_rows * 8; }
 
 void seq_attn_fwd(SeqAttn a, void* workspace, hipStream_t st) {
   a.splits = splits(a);
