@@ -375,53 +375,45 @@ def mrem_queue_entry(q, age: int):
 # ------------------------------------------------------------------------------
 
 _DTYPES = {torch.bfloat16: MREM_BF16, torch.float32: MREM_FP32}
+_TYPES = {v: k for k, v in _DTYPES.items()}
 
 
-def _fit(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
-
-
-def _heads(t: torch.Tensor, name: str) -> int:
-    """Address of a [rows, heads, head_dim] view whose heads are contiguous; rows may lie any distance apart."""
-    _fit(t.dim() == 3 and t.dtype in _DTYPES, f"{name}: bf16 or fp32 [rows, heads, head_dim] expected")
-    _fit(t.numel() == 0 or ((t.stride(2) == 1 or t.shape[2] == 1) and (t.stride(1) == t.shape[2] or t.shape[1] == 1)), f"{name}: the heads of a row must be contiguous")
-    return t.data_ptr() or None
+def _heads(t: torch.Tensor, name: str) -> None:
+    """t is a [rows, heads, head_dim] view whose heads are contiguous; rows may lie any distance apart."""
+    if t.dim() != 3 or t.dtype not in _DTYPES:
+        raise ValueError(f"{name}: bf16 or fp32 [rows, heads, head_dim] expected")
+    if t.numel() and not ((t.stride(2) == 1 or t.shape[2] == 1) and (t.stride(1) == t.shape[2] or t.shape[1] == 1)):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
 
 
 def _row_stride(t: torch.Tensor) -> int:
     """Elements between rows; of a single row or none, its width."""
-    return t.stride(0) if t.shape[0] > 1 else t[0].numel() if t.shape[0] else t.shape[1:].numel()
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1:].numel()
 
 
-def _plain(t: Optional[torch.Tensor], name: str, dtype, shape) -> Optional[int]:
+def _plain(t: Optional[torch.Tensor], name: str, dtype, shape):
+    """Address of a contiguous tensor of that type and shape, or None for None and for an empty one."""
     if t is None:
         return None
-    _fit(t.dtype == dtype and tuple(t.shape) == tuple(shape), f"{name}: {dtype} {tuple(shape)} expected, got {t.dtype} {tuple(t.shape)}")
-    _fit(t.is_contiguous(), f"{name}: contiguous tensor required")
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: {dtype} {shape} expected, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous tensor required")
     return t.data_ptr() or None
 
 
-class _on:
-    """The device that all the tensors are on is the current one inside; gives the stream for it."""
-
-    def __init__(self, stream, *tensors):
-        devices = {t.device for t in tensors if t is not None}
-        _fit(len(devices) == 1, f"the tensors are on several devices: {sorted(map(str, devices))}")
-        (self.device,) = devices
-        _fit(self.device.type == "cuda", "device tensors required")
-        self.stream = stream
-        self.guard = None
-
-    def __enter__(self):
-        if self.device.index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(self.device)
-            self.guard.__enter__()
-        return _stream(self.stream)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _run(fn, stream, tensors, *args) -> None:
+    """fn(*args, stream) on the tensors' device, where it is not the current one too."""
+    device = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"the tensors are on several devices: {sorted({str(t.device) for t in tensors if t is not None})}")
+    if device < 0:
+        raise ValueError("device tensors required")
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _check(fn(*args, _stream(stream)))
+    _check(fn(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)))
 
 
 def mrem_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int = MREM_ROTARY_PLAIN, factor: float = 1.0,
@@ -433,13 +425,15 @@ def mrem_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int
 
 
 def _rotary(fn, x, y, rotary_dim, interleaved, amplitude, freq, positions, seq, stream):
-    xp, yp = _heads(x, "x"), _heads(y, "y")
-    _fit(x.shape == y.shape and x.dtype == y.dtype, "x and y must have one shape and type")
-    fp = _plain(freq, "freq", torch.float64, (rotary_dim // 2,))
-    pp = _plain(positions, "positions", torch.int32, (x.shape[0],))
-    with _on(stream, x, y, freq, positions) as st:
-        _check(fn(xp, yp, _DTYPES[x.dtype], x.shape[0], x.shape[1], x.shape[2], _row_stride(x), _row_stride(y), rotary_dim, int(interleaved),
-                  amplitude, fp, pp, x.shape[0] or 1 if seq is None else seq, st))
+    _heads(x, "x")
+    _heads(y, "y")
+    shape = x.shape
+    if y.shape != shape or y.dtype is not x.dtype:
+        raise ValueError("x and y must have one shape and type")
+    rows, heads, dim = shape
+    _run(fn, stream, (x, y, freq, positions), x.data_ptr() or None, y.data_ptr() or None, _DTYPES[x.dtype], rows, heads, dim, _row_stride(x),
+         _row_stride(y), rotary_dim, int(interleaved), amplitude, _plain(freq, "freq", torch.float64, (rotary_dim // 2,)),
+         _plain(positions, "positions", torch.int32, (rows,)), (rows or 1) if seq is None else seq)
 
 
 def mrem_rotary_forward(x, y, rotary_dim, interleaved, amplitude, freq, positions=None, seq=None, stream=None) -> None:
@@ -455,8 +449,10 @@ def attention_config(q, k, v, out, batch: int, causal: int = 0, window: int = 0,
     """The config of calls on tensors like these ([rows, heads, head_dim]); scale: head_dim^-0.5 if None."""
     for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
         _heads(t, name)
-        _fit(t.dtype == q.dtype and t.shape[2] == q.shape[2], f"{name}: q's type and head_dim expected")
-    _fit(k.shape == v.shape and q.shape == out.shape, "k and v, and q and out, must have one shape")
+        if t.dtype is not q.dtype or t.shape[2] != q.shape[2]:
+            raise ValueError(f"{name}: q's type and head_dim expected")
+    if k.shape != v.shape or q.shape != out.shape:
+        raise ValueError("k and v, and q and out, must have one shape")
     return mrem_attention_config(dtype=_DTYPES[q.dtype], batch=batch, q_heads=q.shape[1], kv_heads=k.shape[1], head_dim=q.shape[2],
                                  causal=int(causal), window=window, scale=q.shape[2] ** -0.5 if scale is None else scale, q_rows=q.shape[0],
                                  k_rows=k.shape[0], ld_q=_row_stride(q), ld_k=_row_stride(k), ld_v=_row_stride(v), ld_out=_row_stride(out))
@@ -466,16 +462,15 @@ def mrem_attention_workspace_bytes(cfg, backward) -> int:
     return _lib.mrem_attention_workspace_bytes(C.byref(cfg), int(bool(backward)))
 
 
-def _attention_tensor(cfg, t, name, rows, heads, ld):
-    p = _heads(t, name)
-    _fit(_DTYPES[t.dtype] == cfg.dtype and tuple(t.shape) == (rows, heads, cfg.head_dim), f"{name}: another type or shape than the config's")
-    _fit(t.shape[0] <= 1 or t.stride(0) == ld, f"{name}: rows {ld} elements apart expected")
-    return p
-
-
-def _attention_sequences(cfg, q_start, k_start, q_len, k_len):
-    n = cfg.batch
-    return [_plain(t, name, torch.int32, (m,)) for t, name, m in ((q_start, "q_start", n + 1), (k_start, "k_start", n + 1), (q_len, "q_len", n), (k_len, "k_len", n))]
+def _rows_like(t, name, dtype, shape, ld):
+    """Address of a tensor that has the config's type and shape and rows ld elements apart."""
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: another type or shape than the config's")
+    if t.stride() != (ld, shape[2], 1):  # unless those that differ are of a single row, head or value
+        _heads(t, name)
+        if t.shape[0] > 1 and t.stride(0) != ld:
+            raise ValueError(f"{name}: rows {ld} elements apart expected")
+    return t.data_ptr() or None
 
 
 def _workspace(t):
@@ -483,27 +478,27 @@ def _workspace(t):
 
 
 def mrem_attention_forward(cfg, q, k, v, q_start, k_start, q_len, k_len, out, lse, workspace, stream=None) -> None:
-    qs, ks = (cfg.q_rows, cfg.q_heads), (cfg.k_rows, cfg.kv_heads)
-    ptrs = [_attention_tensor(cfg, q, "q", *qs, cfg.ld_q), _attention_tensor(cfg, k, "k", *ks, cfg.ld_k), _attention_tensor(cfg, v, "v", *ks, cfg.ld_v)]
-    outs = [_attention_tensor(cfg, out, "out", *qs, cfg.ld_out), _plain(lse, "lse", torch.float32, (cfg.q_heads, cfg.q_rows))]
-    seqs = _attention_sequences(cfg, q_start, k_start, q_len, k_len)
-    with _on(stream, q, k, v, q_start, k_start, q_len, k_len, out, lse, workspace) as st:
-        _check(_lib.mrem_attention_forward(C.byref(cfg), *ptrs, *seqs, *outs, *_workspace(workspace), st))
+    ty, d, n, hq, qr = _TYPES.get(cfg.dtype), cfg.head_dim, cfg.batch, cfg.q_heads, cfg.q_rows
+    qs, ks, i32 = (qr, hq, d), (cfg.k_rows, cfg.kv_heads, d), torch.int32
+    _run(_lib.mrem_attention_forward, stream, (q, k, v, q_start, k_start, q_len, k_len, out, lse, workspace), C.byref(cfg),
+         _rows_like(q, "q", ty, qs, cfg.ld_q), _rows_like(k, "k", ty, ks, cfg.ld_k), _rows_like(v, "v", ty, ks, cfg.ld_v),
+         _plain(q_start, "q_start", i32, (n + 1,)), _plain(k_start, "k_start", i32, (n + 1,)), _plain(q_len, "q_len", i32, (n,)),
+         _plain(k_len, "k_len", i32, (n,)), _rows_like(out, "out", ty, qs, cfg.ld_out), _plain(lse, "lse", torch.float32, (hq, qr)), *_workspace(workspace))
 
 
 def mrem_attention_backward(cfg, q, k, v, out, lse, d_out, q_start, k_start, q_len, k_len, dq, dk, dv, workspace, stream=None) -> None:
-    qs, ks = (cfg.q_rows, cfg.q_heads), (cfg.k_rows, cfg.kv_heads)
-    ptrs = [_attention_tensor(cfg, q, "q", *qs, cfg.ld_q), _attention_tensor(cfg, k, "k", *ks, cfg.ld_k), _attention_tensor(cfg, v, "v", *ks, cfg.ld_v),
-            _attention_tensor(cfg, out, "out", *qs, cfg.ld_out), _plain(lse, "lse", torch.float32, (cfg.q_heads, cfg.q_rows)),
-            _attention_tensor(cfg, d_out, "d_out", *qs, cfg.ld_out)]
-    outs = [_attention_tensor(cfg, dq, "dq", *qs, cfg.ld_q), _attention_tensor(cfg, dk, "dk", *ks, cfg.ld_k), _attention_tensor(cfg, dv, "dv", *ks, cfg.ld_v)]
-    seqs = _attention_sequences(cfg, q_start, k_start, q_len, k_len)
-    with _on(stream, q, k, v, out, lse, d_out, q_start, k_start, q_len, k_len, dq, dk, dv, workspace) as st:
-        _check(_lib.mrem_attention_backward(C.byref(cfg), *ptrs, *seqs, *outs, *_workspace(workspace), st))
+    ty, d, n, hq, qr = _TYPES.get(cfg.dtype), cfg.head_dim, cfg.batch, cfg.q_heads, cfg.q_rows
+    qs, ks, i32, ld_q, ld_k, ld_v, ld_out = (qr, hq, d), (cfg.k_rows, cfg.kv_heads, d), torch.int32, cfg.ld_q, cfg.ld_k, cfg.ld_v, cfg.ld_out
+    _run(_lib.mrem_attention_backward, stream, (q, k, v, out, lse, d_out, q_start, k_start, q_len, k_len, dq, dk, dv, workspace), C.byref(cfg),
+         _rows_like(q, "q", ty, qs, ld_q), _rows_like(k, "k", ty, ks, ld_k), _rows_like(v, "v", ty, ks, ld_v), _rows_like(out, "out", ty, qs, ld_out),
+         _plain(lse, "lse", torch.float32, (hq, qr)), _rows_like(d_out, "d_out", ty, qs, ld_out), _plain(q_start, "q_start", i32, (n + 1,)),
+         _plain(k_start, "k_start", i32, (n + 1,)), _plain(q_len, "q_len", i32, (n,)), _plain(k_len, "k_len", i32, (n,)),
+         _rows_like(dq, "dq", ty, qs, ld_q), _rows_like(dk, "dk", ty, ks, ld_k), _rows_like(dv, "dv", ty, ks, ld_v), *_workspace(workspace))
 
 
 def _logits(t, name):
-    _fit(t.dim() == 2 and t.dtype in _DTYPES and (t.stride(1) == 1 or t.shape[1] == 1), f"{name}: bf16 or fp32 [rows, vocab] with contiguous rows expected")
+    if t.dim() != 2 or t.dtype not in _DTYPES or not (t.stride(1) == 1 or t.shape[1] == 1):
+        raise ValueError(f"{name}: bf16 or fp32 [rows, vocab] with contiguous rows expected")
     return t.data_ptr() or None
 
 
@@ -511,17 +506,19 @@ def mrem_distill_loss(logits, top_logits, top_index, teacher_lse, temperature, r
     """logits, grad: [rows, vocab], rows any distance apart; teacher_lse, row_weight, loss_out and grad may be None."""
     xp = _logits(logits, "logits")
     rows, vocab = logits.shape
-    _fit(top_logits.dim() == 2, "top_logits: [rows, k] expected")
-    k = top_logits.shape[1]
+    if top_logits.dim() != 2:
+        raise ValueError("top_logits: [rows, k] expected")
+    k, f32 = top_logits.shape[1], torch.float32
     gp, ld_grad = None, vocab
     if grad is not None:
         gp, ld_grad = _logits(grad, "grad"), _row_stride(grad)
-        _fit(grad.shape == logits.shape and grad.dtype == logits.dtype, "grad: the logits' shape and type expected")
-    args = [_plain(top_logits, "top_logits", torch.float32, (rows, k)), _plain(top_index, "top_index", torch.int32, (rows, k)), k,
-            _plain(teacher_lse, "teacher_lse", torch.float32, (rows,)), temperature, _plain(row_weight, "row_weight", torch.float32, (rows,)), scale,
-            _plain(loss_rows, "loss_rows", torch.float32, (rows,)), _plain(loss_out, "loss_out", torch.float32, (1,))]
-    with _on(stream, logits, top_logits, top_index, teacher_lse, row_weight, loss_rows, loss_out, grad) as st:
-        _check(_lib.mrem_distill_loss(xp, _DTYPES[logits.dtype], rows, vocab, _row_stride(logits), *args, gp, ld_grad, st))
+        if grad.shape != logits.shape or grad.dtype is not logits.dtype:
+            raise ValueError("grad: the logits' shape and type expected")
+    _run(_lib.mrem_distill_loss, stream, (logits, top_logits, top_index, teacher_lse, row_weight, loss_rows, loss_out, grad), xp,
+         _DTYPES[logits.dtype], rows, vocab, _row_stride(logits), _plain(top_logits, "top_logits", f32, (rows, k)),
+         _plain(top_index, "top_index", torch.int32, (rows, k)), k, _plain(teacher_lse, "teacher_lse", f32, (rows,)), temperature,
+         _plain(row_weight, "row_weight", f32, (rows,)), scale, _plain(loss_rows, "loss_rows", f32, (rows,)), _plain(loss_out, "loss_out", f32, (1,)),
+         gp, ld_grad)
 
 
 # ------------------------------------------------------------------------------

@@ -139,48 +139,48 @@ __device__ __forceinline__ float other_half(float v) {
 struct Seq {
   int64_t q0, k0;  // first rows
   int qn, kn;
+  int b, tile;
 };
-__device__ __forceinline__ int64_t start_of(const int32_t* start, int64_t rows, int batch, int b) {
-  return start ? min(max((int64_t)start[b], (int64_t)0), rows) : (rows / batch) * b;
+__device__ __forceinline__ int64_t uniform(int64_t v, int lane) {
+  return ((int64_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) | (unsigned)__builtin_amdgcn_readlane((int)v, lane);
 }
-__device__ __forceinline__ void sequence_rows(const int32_t* start, const int32_t* len, int64_t rows, int batch, int b, int64_t* first, int* n) {
-  const int64_t lo = start_of(start, rows, batch, b), hi = max(start_of(start, rows, batch, b + 1), lo);
-  const int64_t m = len ? min(max((int64_t)len[b], (int64_t)0), hi - lo) : hi - lo;
-  // the same for the whole block: kept in scalar registers
-  *first = ((int64_t)__builtin_amdgcn_readfirstlane((int)(lo >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)lo);
-  *n = __builtin_amdgcn_readfirstlane((int)m);
-}
-__device__ __forceinline__ Seq sequence(const SeqAttn& a, int b) {
-  Seq s;
-  sequence_rows(a.q_start, a.q_len, a.q_rows, a.batch, b, &s.q0, &s.qn);
-  sequence_rows(a.k_start, a.k_len, a.k_rows, a.batch, b, &s.k0, &s.kn);
-  return s;
-}
-// sequence and tile of a slot; `per` rows of an axis a row of the tensor, `tile` rows a tile
-__device__ __forceinline__ int slot_sequence(const int32_t* start, int64_t rows, int batch, int per, int tile, int slot, int* tile_index) {
-  int b = -1;
-  if (!start) {
-    // base(b) = b * each / tile + b is a known line: from a guess that is at most one too low
-    const int64_t each = rows / batch * per;
-    int64_t g = (int64_t)slot * tile / (each + tile);
-    while (g + 1 < batch && (g + 1) * each / tile + g + 1 <= slot) ++g;
-    b = (int)min(g, (int64_t)batch - 1);
-  } else {
-    // a wavefront looks at 64 sequences at a time: the last one whose first slot is not behind this one
-    const int lane = threadIdx.x & (kWave - 1);
-    for (int at = 0; at < batch; at += kWave) {
-      const int i = at + lane;
-      const bool before = i < batch && start_of(start, rows, batch, min(i, batch)) * per / tile + i <= slot;
-      const unsigned long long m = __ballot(before);
-      if (!m) break;
-      b = at + 63 - __builtin_clzll(m);
-    }
-    b = max(b, 0);
+struct Rows {
+  int64_t first, end;  // of a sequence, cut to the rows that there are
+  __device__ __forceinline__ Rows(const int32_t* start, const int32_t* len, int64_t rows, int batch, int b) {
+    first = start ? min(max((int64_t)start[b], (int64_t)0), rows) : rows / batch * b;
+    end = start ? max(min((int64_t)start[b + 1], rows), first) : first + rows / batch;
+    if (len) end = min(end, first + max(len[b], 0));
   }
-  b = __builtin_amdgcn_readfirstlane(b);
-  const int64_t base = start_of(start, rows, batch, b) * per / tile + b;
-  *tile_index = __builtin_amdgcn_readfirstlane((int)(slot - base));
-  return b;
+};
+// The sequence and the tile of a slot of the queries' axis (or the keys'), `per` rows of it a row of the tensor, `tile` rows a tile.
+// A wavefront looks at 64 sequences at a time, for the last one whose first slot is not behind this one; a lane loads all that
+// there is to know about its sequence at once, so that up to 64 of them cost one trip to memory.
+template <bool KEYS>
+__device__ __forceinline__ Seq find_sequence(const SeqAttn& a, int per, int tile, int slot) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int32_t* start = KEYS ? a.k_start : a.q_start;
+  int at = 0;
+  if (!start) {  // first slots lie on a known line: from a guess that is at most a few too low
+    const int64_t each = (KEYS ? a.k_rows : a.q_rows) / a.batch * per;
+    at = (int)min((int64_t)slot * tile / (each + tile), (int64_t)a.batch - 1);
+  }
+  Seq s{};
+  for (; at < a.batch; at += kWave) {
+    const int i = min(at + lane, a.batch - 1);
+    const Rows q(a.q_start, a.q_len, a.q_rows, a.batch, i), k(a.k_start, a.k_len, a.k_rows, a.batch, i);
+    const int64_t base = (KEYS ? k.first : q.first) * per / tile + i;
+    const unsigned long long before = __ballot(at + lane < a.batch && base <= slot);
+    if (!before) break;
+    const int from = 63 - __builtin_clzll(before);
+    s.q0 = uniform(q.first, from);
+    s.k0 = uniform(k.first, from);
+    s.qn = (int)(uniform(q.end, from) - s.q0);
+    s.kn = (int)(uniform(k.end, from) - s.k0);
+    s.b = at + from;
+    s.tile = (int)(slot - uniform(base, from));
+    if (from < 63) break;
+  }
+  return s;
 }
 int64_t slots(int64_t rows, int batch, int per, int tile) { return rows * per / tile + batch; }
 
@@ -289,13 +289,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_fwd_k(Se
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = a.hq / a.hk;
   const int head = blockIdx.x % a.hk, split = blockIdx.y;
-  int tile;
   // the last tiles see the most keys: they go first
   const int slot = (int)(gridDim.x / a.hk - 1 - blockIdx.x / a.hk);
-  const int b = slot_sequence(a.q_start, a.q_rows, a.batch, group, RB, slot, &tile);
-  const Seq s = sequence(a, b);
-  const int rows = s.qn * group, r0 = tile * RB;
-  if (tile < 0 || r0 >= rows) return;
+  const Seq s = find_sequence<false>(a, group, RB, slot);
+  const int rows = s.qn * group, r0 = s.tile * RB;
+  if (r0 >= rows) return;
 
   const int row = r0 + (RB == 32 ? 0 : 32 * wave) + col, rc = min(row, rows - 1), token = rc / group, h = head * group + rc - token * group;
   const T* q = static_cast<const T*>(a.q) + (s.q0 + token) * a.ld_q + h * D + 8 * half;
@@ -440,15 +438,12 @@ template <class T, int D>
 __global__ __launch_bounds__(kThreads) void seq_join_k(SeqAttn a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = a.hq / a.hk, head = blockIdx.x % a.hk;
   constexpr int RB = 32;
-  int tile;
-  const int b = slot_sequence(a.q_start, a.q_rows, a.batch, group, RB, (int)(blockIdx.x / a.hk), &tile);
-  const Seq s = sequence(a, b);
+  const Seq s = find_sequence<false>(a, group, RB, (int)(blockIdx.x / a.hk));
   const int rows = s.qn * group;
-  if (tile < 0) return;
   const float* ml = a.part + (int64_t)a.splits * a.hq * a.q_rows * D;
   const int64_t step = (int64_t)a.hq * a.q_rows;
   const float c = a.scale * kLog2e;
-  for (int row = tile * RB + wave; row < min(rows, (tile + 1) * RB); row += kWaves) {
+  for (int row = s.tile * RB + wave; row < min(rows, (s.tile + 1) * RB); row += kWaves) {
     const int token = row / group, h = head * group + row - token * group;
     const int64_t at = (int64_t)h * a.q_rows + s.q0 + token;
     float m = -INFINITY;
@@ -483,12 +478,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_bwd_q_k(
   __shared__ __attribute__((aligned(16))) T Vs[KT * S];
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = a.hq / a.hk, head = blockIdx.x % a.hk;
-  int tile;
   const int slot = (int)(gridDim.x / a.hk - 1 - blockIdx.x / a.hk);
-  const int b = slot_sequence(a.q_start, a.q_rows, a.batch, group, RB, slot, &tile);
-  const Seq s = sequence(a, b);
-  const int rows = s.qn * group, r0 = tile * RB;
-  if (tile < 0 || r0 >= rows) return;
+  const Seq s = find_sequence<false>(a, group, RB, slot);
+  const int rows = s.qn * group, r0 = s.tile * RB;
+  if (r0 >= rows) return;
 
   const int row = r0 + 32 * wave + col, rc = min(row, rows - 1), token = rc / group, h = head * group + rc - token * group;
   const T* q = static_cast<const T*>(a.q) + (s.q0 + token) * a.ld_q + h * D + 8 * half;
@@ -585,12 +578,10 @@ __global__ __launch_bounds__(kThreads* kRowParts<T>, kRowParts<T>) void seq_bwd_
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = w % kWaves, part = w / kWaves;
   const int group = a.hq / a.hk, head = blockIdx.x % a.hk;
-  int tile;
   const int slot = (int)(blockIdx.x / a.hk);  // the first keys are seen by the most queries
-  const int b = slot_sequence(a.k_start, a.k_rows, a.batch, 1, RB, slot, &tile);
-  const Seq s = sequence(a, b);
-  const int j0 = tile * RB;
-  if (tile < 0 || j0 >= s.kn) return;
+  const Seq s = find_sequence<true>(a, 1, RB, slot);
+  const int j0 = s.tile * RB;
+  if (j0 >= s.kn) return;
 
   const int key = j0 + 32 * wave + col, kc = min(key, s.kn - 1);
   const T* kp = static_cast<const T*>(a.k) + (s.k0 + kc) * a.ld_k + head * D + 8 * half;
