@@ -1499,6 +1499,7 @@ static mrem_status attention_shape(const char* who, const mrem_attention_config*
   *a = SeqAttn{};
   a->dt = dt_of(c.dtype); a->batch = c.batch; a->hq = c.q_heads; a->hk = c.kv_heads; a->d = c.head_dim;
   a->causal = c.causal; a->window = c.window; a->scale = c.scale;
+  a->group = Divisor(c.q_heads / c.kv_heads); a->q_each = c.q_rows / c.batch; a->k_each = c.k_rows / c.batch;
   a->q_rows = c.q_rows; a->k_rows = c.k_rows; a->ld_q = c.ld_q; a->ld_k = c.ld_k; a->ld_v = c.ld_v; a->ld_o = c.ld_out;
   return MREM_OK;
 }

@@ -322,6 +322,21 @@ void reduce_and_step(const ReduceJob& other, const ReduceJob& grad, float* p, fl
 void rotary(int dt, const void* x, void* y, int64_t rows, int heads, int dim, int64_t ld_x, int64_t ld_y, int rotary_dim, bool interleaved,
             float amplitude, float sign, const double* freq, const int32_t* positions, int64_t seq, hipStream_t st);
 
+// x / d of 0 <= x < 2^31 by a multiplication: with l = ceil(log2 d), mul = ceil(2^(31 + l) / d) < 2^32 and the quotient is x mul >> 31 + l
+// (the error of mul is under 1 and x under 2^31, so that of the product is under 2^(31 + l) / d)
+struct Divisor {
+  unsigned mul = 0;
+  int shift = 0, d = 1;
+  Divisor() = default;
+  explicit Divisor(int by) : d(by) {
+    int l = 0;
+    while (((int64_t)1 << l) < by) ++l;
+    mul = (unsigned)((((uint64_t)1 << (31 + l)) + by - 1) / by);
+    shift = l;
+  }
+  __device__ __forceinline__ int of(int x) const { return (int)(((uint64_t)(unsigned)x * mul) >> 31 >> shift); }
+};
+
 // Tensors and sequences of one attention call; see the header of the ABI.
 struct SeqAttn {
   int dt, batch, hq, hk, d, causal, window;
@@ -334,6 +349,8 @@ struct SeqAttn {
   const int32_t *q_start, *k_start, *q_len, *k_len;
   float* part;  // partial results of keys shared out among blocks
   int splits;
+  Divisor group;             // hq / hk
+  int64_t q_each, k_each;    // rows of a sequence where there are no starts
 };
 size_t seq_attn_fwd_bytes(const SeqAttn& a);
 size_t seq_attn_bwd_bytes(const SeqAttn& a);

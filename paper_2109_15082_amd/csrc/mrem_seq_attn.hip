@@ -30,9 +30,25 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kThreads = 256, kWaves = 4;
 
-// elements of a row of an LDS tile: 16 bytes more than the row, so that neither row nor column reads meet in a bank
+// Tiles in LDS.  They are read by rows (16 lanes, 16 consecutive rows, 16 bytes each) and down their columns (4 consecutive rows, 64 bytes
+// each).  bf16: rows follow each other without a gap and the 16-byte pieces of a row are exchanged by an exclusive or with a number of
+// the row, such that either access meets all 64 banks once: rows lie 16, 8 or 4 pieces apart, of which 16 are the banks, so the number's
+// upper bits follow the row's lowest ones, which a column access counts through, and its two lowest bits the next ones.  (A gap of 16
+// bytes a row instead serves the rows but lets the four rows of a column access meet.)  fp32: columns are read value by value; a gap.
 template <class T, int D>
-constexpr int kStride = D + 16 / (int)sizeof(T);
+constexpr int kStride = sizeof(T) == 2 ? D : D + 16 / (int)sizeof(T);
+template <class T, int D>
+__device__ __forceinline__ int piece_of(int row) {
+  if constexpr (sizeof(T) == 4) return 0;
+  else if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+  else if constexpr (D == 64) return ((row & 2) << 1) | ((row >> 2) & 3);
+  else return (row >> 2) & 3;
+}
+// element `col` of a row; pieces are whole: col may be advanced within its piece
+template <class T, int D>
+__device__ __forceinline__ int lds_at(int row, int col) {
+  return row * kStride<T, D> + (col ^ (piece_of<T, D>(row) * (16 / (int)sizeof(T))));
+}
 
 // ---- fragments: 8 values a lane, contraction index 8 (lane / 32) + i ---------
 template <class T>
@@ -79,26 +95,17 @@ __device__ __forceinline__ Frag<T> load8(const T* p) {
   }
   return f;
 }
-// fragment down the rows of an LDS tile: column c0 + lane % 32, rows first + 0..3 and second + 0..3
-template <class T, int D>
-__device__ __forceinline__ Frag<T> load_cols(const T* tile, int c0, int first, int second, int lane) {
-  Frag<T> f;
-  if constexpr (sizeof(T) == 2) {
-    const int g = lane >> 4, s = lane & 15;
-    const T* p = tile + (s >> 2) * kStride<T, D> + c0 + 16 * (g & 1) + 4 * (s & 3);
-    union { bf16x8_t v; s16x4_t h[2]; } u;
-    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p + first * kStride<T, D>));
-    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p + second * kStride<T, D>));
-    f.v = u.v;
-  } else {
-    const T* p = tile + c0 + (lane & 31);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f.v[i] = p[(first + i) * kStride<T, D>];
-      f.v[4 + i] = p[(second + i) * kStride<T, D>];
-    }
-  }
-  return f;
+// Where a lane reads a bf16 tile (at a multiple of 256 bytes), as an address whose exclusive or with a constant is another piece of the
+// same row.  Forgotten by the compiler how it came about: it would keep each of those pieces' addresses in a register of its own throughout a loop.
+typedef __attribute__((address_space(3))) char lds_char_t;
+__device__ __forceinline__ unsigned lane_address(const bf16_t* tile, int offset) {
+  unsigned a = (unsigned)(size_t)(lds_char_t*)tile + 2 * offset;
+  asm("" : "+v"(a));
+  return a;
+}
+__device__ __forceinline__ bf16x8_t read8(unsigned a) { return *(const __attribute__((address_space(3))) bf16x8_t*)(size_t)a; }
+__device__ __forceinline__ s16x4_t read_tr(unsigned a) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(size_t)a);
 }
 // accumulator registers 8 s .. 8 s + 7 as an operand.  bf16: probabilities and score gradients are rounded once, to 8 bits of
 // mantissa, as the values of the products around them are; what is added up stays in 32 bits
@@ -109,26 +116,60 @@ __device__ __forceinline__ Frag<T> from_acc(const f32x16_t& a, int s) {
   for (int i = 0; i < 8; ++i) f.v[i] = static_cast<T>(a[8 * s + i]);
   return f;
 }
-// 32 x 32 tile: LDS rows [row0, row0 + 32) times the 32 rows held as fragments
-template <class T, int D>
-__device__ __forceinline__ f32x16_t rows_times(const T* tile, int row0, int lane, const Frag<T> (&b)[D / 16]) {
+// 32 x 32 tile: LDS rows [row0, row0 + 32) times the 32 rows held as fragments b(kk), 16 columns each
+template <class T, int D, class B>
+__device__ __forceinline__ f32x16_t rows_times(const T* tile, int row0, int lane, B b) {
   f32x16_t acc = zero16();
-  const T* p = tile + (row0 + (lane & 31)) * kStride<T, D> + (lane >> 5) * 8;
+  const int row = row0 + (lane & 31), at = lds_at<T, D>(row, 8 * (lane >> 5));
+  if constexpr (sizeof(T) == 2) {
+    const unsigned a = lane_address(tile, at);
 #pragma unroll
-  for (int kk = 0; kk < D / 16; ++kk) acc = mma(load8(p + 16 * kk), b[kk], acc);
+    for (int kk = 0; kk < D / 16; ++kk) acc = mma(Frag<T>{read8(a ^ (32 * kk))}, b(kk), acc);
+  } else {
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) acc = mma(load8(tile + at + 16 * kk), b(kk), acc);
+  }
   return acc;
 }
-// acc[e][.] += sum over the tile's 32 rows of tile[row][e] w[row], w in accumulator order
+// acc[e][.] += sum over the tile's 32 rows of tile[row][e] w[row], w in accumulator order: the tile's fragments run down its rows, column
+// 32 e + lane % 32, rows 16 s + 4 (lane / 32) + 0..3 and 8 more
 template <class T, int D>
 __device__ __forceinline__ void add_rows(f32x16_t (&acc)[D / 32], const T* tile, int row0, int lane, const f32x16_t& w) {
+  if constexpr (sizeof(T) == 2) {
+    // the transposing read: in a group of 16 lanes, lane s names columns 4 (s % 4) .. + 3 of row s / 4 and receives column s of the four rows
+    const int g = lane >> 4, s16 = lane & 15, row = row0 + 4 * (lane >> 5) + (s16 >> 2), col = 16 * (g & 1) + 4 * (s16 & 3);
+    const unsigned a = lane_address(tile, lds_at<T, D>(row, col));
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const Frag<T> f = from_acc<T>(w, s);
-    const int r = row0 + 16 * s + 4 * (lane >> 5);
+    for (int s = 0; s < 2; ++s) {
+      const Frag<T> f = from_acc<T>(w, s);
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) acc[e] = mma(load_cols<T, D>(tile, 32 * e, r, r + 8, lane), f, acc[e]);
+      for (int e = 0; e < D / 32; ++e) {
+        union { bf16x8_t v; s16x4_t h[2]; } u;
+        u.h[0] = read_tr((a ^ (64 * e)) + 32 * s * D);
+        u.h[1] = read_tr((a ^ (64 * e) ^ 32) + (32 * s + 16) * D);  // 8 rows on: piece_of differs in its bit 1
+        acc[e] = mma(Frag<T>{u.v}, f, acc[e]);
+      }
+    }
+  } else {
+    const T* p = tile + (row0 + 4 * (lane >> 5)) * kStride<T, D> + (lane & 31);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const Frag<T> f = from_acc<T>(w, s);
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) {
+        Frag<T> u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u.v[i] = p[(16 * s + i) * kStride<T, D> + 32 * e];
+          u.v[4 + i] = p[(16 * s + 8 + i) * kStride<T, D> + 32 * e];
+        }
+        acc[e] = mma(u, f, acc[e]);
+      }
+    }
   }
 }
+// LDS accesses of a wavefront are carried out in order: nothing is to be moved across, that is all
+__device__ __forceinline__ void wave_fence() { asm volatile("" ::: "memory"); }
 // the other half wavefront's value
 __device__ __forceinline__ float other_half(float v) {
   const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -146,9 +187,9 @@ __device__ __forceinline__ int64_t uniform(int64_t v, int lane) {
 }
 struct Rows {
   int64_t first, end;  // of a sequence, cut to the rows that there are
-  __device__ __forceinline__ Rows(const int32_t* start, const int32_t* len, int64_t rows, int batch, int b) {
-    first = start ? min(max((int64_t)start[b], (int64_t)0), rows) : rows / batch * b;
-    end = start ? max(min((int64_t)start[b + 1], rows), first) : first + rows / batch;
+  __device__ __forceinline__ Rows(const int32_t* start, const int32_t* len, int64_t rows, int64_t each, int b) {
+    first = start ? min(max((int64_t)start[b], (int64_t)0), rows) : each * b;
+    end = start ? max(min((int64_t)start[b + 1], rows), first) : first + each;
     if (len) end = min(end, first + max(len[b], 0));
   }
 };
@@ -160,14 +201,15 @@ __device__ __forceinline__ Seq find_sequence(const SeqAttn& a, int per, int tile
   const int lane = threadIdx.x & (kWave - 1);
   const int32_t* start = KEYS ? a.k_start : a.q_start;
   int at = 0;
-  if (!start) {  // first slots lie on a known line: from a guess that is at most a few too low
-    const int64_t each = (KEYS ? a.k_rows : a.q_rows) / a.batch * per;
-    at = (int)min((int64_t)slot * tile / (each + tile), (int64_t)a.batch - 1);
+  if (!start) {  // first slots lie on a known line: from a guess that is never too high
+    // (in 32 bits of a product and a quotient of up to 2^24: off by less than 8)
+    const float guess = (float)slot * (float)tile / ((float)((KEYS ? a.k_each : a.q_each) * per) + (float)tile);
+    at = min(max((int)guess - 8, 0), a.batch - 1);
   }
   Seq s{};
   for (; at < a.batch; at += kWave) {
     const int i = min(at + lane, a.batch - 1);
-    const Rows q(a.q_start, a.q_len, a.q_rows, a.batch, i), k(a.k_start, a.k_len, a.k_rows, a.batch, i);
+    const Rows q(a.q_start, a.q_len, a.q_rows, a.q_each, i), k(a.k_start, a.k_len, a.k_rows, a.k_each, i);
     const int64_t base = (KEYS ? k.first : q.first) * per / tile + i;
     const unsigned long long before = __ballot(at + lane < a.batch && base <= slot);
     if (!before) break;
@@ -208,7 +250,7 @@ struct Stage {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int q = threadIdx.x + i * kThreads, row = q / kRowPieces;
-      if (kAll % kThreads == 0 || q < kAll) *reinterpret_cast<u32x4_t*>(dst + row * kStride<T, D> + q % kRowPieces * kPiece) = j0 + row < n ? v[i] : u32x4_t{0u, 0u, 0u, 0u};
+      if (kAll % kThreads == 0 || q < kAll) *reinterpret_cast<u32x4_t*>(dst + lds_at<T, D>(row, q % kRowPieces * kPiece)) = j0 + row < n ? v[i] : u32x4_t{0u, 0u, 0u, 0u};
     }
   }
 };
@@ -221,12 +263,12 @@ struct QueryRows {
   int token[kN];
   int head[kN];
   u32x4_t q[kN], c[kN];
-  __device__ __forceinline__ void start(int group, int r0) {
+  __device__ __forceinline__ void start(const Divisor& group, int r0) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int row = r0 + threadIdx.x / kRowPieces + i * kApart, t = row / group;
+      const int row = r0 + threadIdx.x / kRowPieces + i * kApart, t = group.of(row);
       token[i] = t;
-      head[i] = row - t * group;
+      head[i] = row - t * group.d;
     }
   }
   // rows r0 + ... of the two tensors (zeros behind n); then the next tile's places
@@ -251,25 +293,46 @@ struct QueryRows {
   __device__ __forceinline__ void store(T* qs, T* cs) const {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int to = (threadIdx.x / kRowPieces + i * kApart) * kStride<T, D> + threadIdx.x % kRowPieces * kPiece;
+      const int to = lds_at<T, D>(threadIdx.x / kRowPieces + i * kApart, threadIdx.x % kRowPieces * kPiece);
       *reinterpret_cast<u32x4_t*>(qs + to) = q[i];
       *reinterpret_cast<u32x4_t*>(cs + to) = c[i];
     }
   }
 };
 
-// a lane's column of a transposed accumulator (32 values of d for each e) to memory as T or fp32
-template <class T, int D>
-__device__ __forceinline__ void store_column(T* p, const f32x16_t (&acc)[D / 32], float f, int half) {
+// A wavefront's transposed tile, a row of 32 in each lane's column, times f, to the rows that `row` gives addresses of (null: not there).
+// bf16 rows are put together in LDS (32 rows of a tile), so that a row leaves in pieces of 16 bytes side by side: written by the lanes
+// that hold them they are pieces of 8 bytes in 32 rows at a time, a quarter of what a store can carry.
+template <class T, int D, class F>
+__device__ __forceinline__ void store_rows(T* scratch, const f32x16_t (&acc)[D / 32], float f, int lane, F row) {
+  const int half = lane >> 5, col = lane & 31;
+  if constexpr (sizeof(T) == 2) {
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e)
+    for (int e = 0; e < D / 32; ++e)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      T* to = p + 32 * e + 8 * i + 4 * half;
-      const float a = acc[e][4 * i] * f, b = acc[e][4 * i + 1] * f, c = acc[e][4 * i + 2] * f, d = acc[e][4 * i + 3] * f;
-      if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4_t*>(to) = bf16x4_t{static_cast<bf16_t>(a), static_cast<bf16_t>(b), static_cast<bf16_t>(c), static_cast<bf16_t>(d)};
-      else *reinterpret_cast<float4*>(to) = make_float4(a, b, c, d);
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<bf16x4_t*>(scratch + lds_at<T, D>(col, 32 * e + 8 * i) + 4 * half) = bf16x4_t{static_cast<bf16_t>(acc[e][4 * i] * f), static_cast<bf16_t>(acc[e][4 * i + 1] * f),
+                                                                    static_cast<bf16_t>(acc[e][4 * i + 2] * f), static_cast<bf16_t>(acc[e][4 * i + 3] * f)};
+    wave_fence();
+    constexpr int kPieces = D / 8, kRows = kWave / kPieces;
+    const int at = lane % kPieces * 8;
+#pragma unroll
+    for (int r = lane / kPieces; r < 32; r += kRows) {
+      const u32x4_t v = *reinterpret_cast<const u32x4_t*>(scratch + lds_at<T, D>(r, at));
+      T* to = row(r);
+      if (to) *reinterpret_cast<u32x4_t*>(to + at) = v;
     }
+    wave_fence();
+  } else {
+    T* to = row(col);
+    if (to) {
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<float4*>(to + 32 * e + 8 * i + 4 * half) = make_float4(acc[e][4 * i] * f, acc[e][4 * i + 1] * f, acc[e][4 * i + 2] * f, acc[e][4 * i + 3] * f);
+    }
+  }
 }
 
 // ---- forward -----------------------------------------------------------------
@@ -278,16 +341,20 @@ __device__ __forceinline__ void store_column(T* p, const f32x16_t (&acc)[D / 32]
 template <class T, int RB>
 constexpr int kKeyTile = RB == 32 ? 128 : sizeof(T) == 2 ? 64 : 32;
 
+// wavefronts a SIMD, by which the registers are bounded
 template <class T, int D, int RB>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_fwd_k(SeqAttn a) {
+constexpr int kForwardWaves = sizeof(T) == 4 ? 1 : D == 128 || RB == 32 ? 2 : 3;
+
+template <class T, int D, int RB>
+__global__ __launch_bounds__(kThreads, (kForwardWaves<T, D, RB>)) void seq_fwd_k(SeqAttn a) {
   constexpr int KT = kKeyTile<T, RB>, NS = RB == 32 ? 1 : KT / 32, S = kStride<T, D>;
   constexpr int kTileBytes = 2 * KT * S * (int)sizeof(T), kMergeBytes = RB == 32 ? 32 * D * 4 * (kWaves - 1) : 0;
-  __shared__ __attribute__((aligned(16))) char lds[kTileBytes > kMergeBytes ? kTileBytes : kMergeBytes];
+  __shared__ __attribute__((aligned(256))) char lds[kTileBytes > kMergeBytes ? kTileBytes : kMergeBytes];
   __shared__ float merge_m[kWaves][32], merge_l[kWaves][32];
   T* Ks = reinterpret_cast<T*>(lds);
   T* Vs = Ks + KT * S;
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int group = a.hq / a.hk;
+  const int group = a.group.d;
   const int head = blockIdx.x % a.hk, split = blockIdx.y;
   // the last tiles see the most keys: they go first
   const int slot = (int)(gridDim.x / a.hk - 1 - blockIdx.x / a.hk);
@@ -295,16 +362,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_fwd_k(Se
   const int rows = s.qn * group, r0 = s.tile * RB;
   if (r0 >= rows) return;
 
-  const int row = r0 + (RB == 32 ? 0 : 32 * wave) + col, rc = min(row, rows - 1), token = rc / group, h = head * group + rc - token * group;
+  const int wr = r0 + (RB == 32 ? 0 : 32 * wave), row = wr + col, rc = min(row, rows - 1), token = a.group.of(rc), h = head * group + rc - token * group;
   const T* q = static_cast<const T*>(a.q) + (s.q0 + token) * a.ld_q + h * D + 8 * half;
   Frag<T> qf[D / 16];
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) qf[kk] = load8(q + 16 * kk);
   const int lo = key_begin(a, s, token), hi = row < rows ? key_end(a, s, token) : 0;
   // of the wavefront's and of the block's rows: keys that any of them sees; all of the wavefront's see [w_lo, w_hi)
-  const int t_first = r0 / group, t_last = (min(r0 + RB, rows) - 1) / group;
+  const int t_first = a.group.of(r0), t_last = a.group.of(min(r0 + RB, rows) - 1);
   int j_lo = key_begin(a, s, t_first), j_hi = key_end(a, s, t_last);
-  const int wr = r0 + (RB == 32 ? 0 : 32 * wave), wt0 = min(wr, rows - 1) / group, wt1 = (min(wr + 32, rows) - 1) / group;
+  const int wt0 = a.group.of(min(wr, rows - 1)), wt1 = a.group.of(min(wr + 32, rows) - 1);
   const int w_lo = key_begin(a, s, wt1), w_hi = key_end(a, s, wt0), any_lo = key_begin(a, s, wt0), any_hi = wr < rows ? key_end(a, s, wt1) : 0;
   if (a.splits > 1) {
     const int n = j_hi > j_lo ? ((j_hi - j_lo + KT - 1) / KT + a.splits - 1) / a.splits * KT : 0;
@@ -336,7 +403,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_fwd_k(Se
     if (j0 + base < any_hi && j0 + base + 32 * NS > any_lo) {
       f32x16_t p[NS];
 #pragma unroll
-      for (int t = 0; t < NS; ++t) p[t] = rows_times<T, D>(Ks, base + 32 * t, lane, qf);
+      for (int t = 0; t < NS; ++t) p[t] = rows_times<T, D>(Ks, base + 32 * t, lane, [&](int kk) { return qf[kk]; });
       // keys of this tile behind the split's last one belong to the next split: it starts at a tile, so none are
       if (j0 + base < w_lo || j0 + base + 32 * NS > w_hi) {
 #pragma unroll
@@ -406,7 +473,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_fwd_k(Se
     for (int e = 0; e < D / 32; ++e)
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[e][r] *= f;
-#pragma unroll
+#pragma unroll 1
     for (int w = 1; w < kWaves; ++w) {
       f = __builtin_amdgcn_exp2f((merge_m[w][col] - mm) * c);
       l += merge_l[w][col] * f;
@@ -418,25 +485,40 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_fwd_k(Se
     }
     m = top;
   }
-  if (row >= rows) return;
-  if (a.splits > 1) {
-    const int64_t at = ((int64_t)split * a.hq + h) * a.q_rows + s.q0 + token;
-    float* ml = a.part + (int64_t)a.splits * a.hq * a.q_rows * D;
-    store_column<float, D>(a.part + at * D, o, 1.f, half);
-    if (half == 0) {
-      ml[2 * at] = m;
-      ml[2 * at + 1] = l;
+  if constexpr (RB == 32) wave_fence();  // the parts have been read
+  const bool whole = a.splits == 1;
+  if (row < rows && half == 0) {
+    const int64_t at = (int64_t)h * a.q_rows + s.q0 + token;
+    if (whole) {
+      a.lse[at] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
+    } else {
+      float* ml = a.part + (int64_t)a.splits * a.hq * a.q_rows * D + 2 * ((int64_t)split * a.hq * a.q_rows + at);
+      ml[0] = m;
+      ml[1] = l;
     }
-    return;
   }
-  store_column<T, D>(static_cast<T*>(a.out) + (s.q0 + token) * a.ld_o + h * D, o, l == 0.f ? 0.f : 1.f / l, half);
-  if (half == 0) a.lse[(int64_t)h * a.q_rows + s.q0 + token] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
+  const auto place = [&](int r, int* head_of, int* token_of) {
+    const int at = wr + r, t = a.group.of(at);
+    *token_of = t;
+    *head_of = head * group + at - t * group;
+    return at < rows;
+  };
+  int rh, rt;
+  if (!whole) {
+    store_rows<float, D>(nullptr, o, 1.f, lane, [&](int r) {
+      return place(r, &rh, &rt) ? a.part + (((int64_t)split * a.hq + rh) * a.q_rows + s.q0 + rt) * D : nullptr;
+    });
+  } else {
+    store_rows<T, D>(reinterpret_cast<T*>(lds) + (RB == 32 ? 0 : wave * 32 * S), o, l == 0.f ? 0.f : 1.f / l, lane, [&](int r) {
+      return place(r, &rh, &rt) ? static_cast<T*>(a.out) + (s.q0 + rt) * a.ld_o + rh * D : nullptr;
+    });
+  }
 }
 
 // joins the parts of a row whose keys were shared out: a wavefront a (token, head)
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void seq_join_k(SeqAttn a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = a.hq / a.hk, head = blockIdx.x % a.hk;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = a.group.d, head = blockIdx.x % a.hk;
   constexpr int RB = 32;
   const Seq s = find_sequence<false>(a, group, RB, (int)(blockIdx.x / a.hk));
   const int rows = s.qn * group;
@@ -444,21 +526,22 @@ __global__ __launch_bounds__(kThreads) void seq_join_k(SeqAttn a) {
   const int64_t step = (int64_t)a.hq * a.q_rows;
   const float c = a.scale * kLog2e;
   for (int row = s.tile * RB + wave; row < min(rows, (s.tile + 1) * RB); row += kWaves) {
-    const int token = row / group, h = head * group + row - token * group;
+    const int token = a.group.of(row), h = head * group + row - token * group;
     const int64_t at = (int64_t)h * a.q_rows + s.q0 + token;
-    float m = -INFINITY;
-    for (int i = 0; i < a.splits; ++i) m = fmaxf(m, ml[2 * (at + i * step)]);
-    const float mm = m == -INFINITY ? 0.f : m;
-    float l = 0.f, o[D / 64 > 0 ? D / 64 : 1] = {};
-    for (int i = 0; i < a.splits; ++i) {
-      const int64_t p = at + i * step;
-      const float part = ml[2 * p + 1], f = __builtin_amdgcn_exp2f((ml[2 * p] - mm) * c);
-      if (part == 0.f) continue;  // no key of its own
-      l += part * f;
+    // a lane a part, of which there are up to 32; a part without a key of its own has the sum 0 and zeros
+    const float2 mine = lane < a.splits ? *reinterpret_cast<const float2*>(ml + 2 * (at + lane * step)) : make_float2(-INFINITY, 0.f);
+    const float m = wave_max(mine.x), weight = mine.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((mine.x - m) * c);
+    const float l = wave_sum(mine.y * weight);
+    float o[D / 64 > 0 ? D / 64 : 1] = {};
+    for (int i0 = 0; i0 < a.splits; i0 += 4)  // four on their way together; weights of parts that there are not are 0
 #pragma unroll
-      for (int e = 0; e < (D + 63) / 64; ++e)
-        if (lane + 64 * e < D) o[e] += a.part[p * D + lane + 64 * e] * f;
-    }
+      for (int k = 0; k < 4; ++k) {
+        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), i0 + k));
+        const float* part = a.part + (at + min(i0 + k, a.splits - 1) * step) * D;
+#pragma unroll
+        for (int e = 0; e < (D + 63) / 64; ++e)
+          if (lane + 64 * e < D) o[e] += part[lane + 64 * e] * w;
+      }
     const float f = l == 0.f ? 0.f : 1.f / l;
     T* out = static_cast<T*>(a.out) + (s.q0 + token) * a.ld_o + h * D;
 #pragma unroll
@@ -471,19 +554,20 @@ __global__ __launch_bounds__(kThreads) void seq_join_k(SeqAttn a) {
 // ---- backward ----------------------------------------------------------------
 // gradient of the queries: 32 rows a wavefront, keys in tiles.  Also leaves delta = out . d_out of each row, formed by the matrix
 // instructions that form d_out . v, so that the two agree to the bit where a query sees one key and its gradient is zero.
-template <class T, int D>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_bwd_q_k(SeqAttn a) {
-  constexpr int RB = 128, KT = kKeyTile<T, RB>, S = kStride<T, D>;
-  __shared__ __attribute__((aligned(16))) T Ks[KT * S];
-  __shared__ __attribute__((aligned(16))) T Vs[KT * S];
+template <class T, int D, int RB>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32 ? 2 : 3) void seq_bwd_q_k(SeqAttn a) {
+  constexpr int KT = kKeyTile<T, RB>, NS = RB == 32 ? 1 : KT / 32, S = kStride<T, D>;
+  static_assert(2 * KT * S * (int)sizeof(T) >= (RB == 32 ? 32 * D * 4 * (kWaves - 1) : 0), "the sums meet where the tiles were");
+  __shared__ __attribute__((aligned(256))) T tiles[2 * KT * S];
+  T *Ks = tiles, *Vs = tiles + KT * S;
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int group = a.hq / a.hk, head = blockIdx.x % a.hk;
+  const int group = a.group.d, head = blockIdx.x % a.hk;
   const int slot = (int)(gridDim.x / a.hk - 1 - blockIdx.x / a.hk);
   const Seq s = find_sequence<false>(a, group, RB, slot);
   const int rows = s.qn * group, r0 = s.tile * RB;
   if (r0 >= rows) return;
 
-  const int row = r0 + 32 * wave + col, rc = min(row, rows - 1), token = rc / group, h = head * group + rc - token * group;
+  const int wr = r0 + (RB == 32 ? 0 : 32 * wave), row = wr + col, rc = min(row, rows - 1), token = a.group.of(rc), h = head * group + rc - token * group;
   const T* q = static_cast<const T*>(a.q) + (s.q0 + token) * a.ld_q + h * D + 8 * half;
   const int64_t o_at = (s.q0 + token) * a.ld_o + h * D + 8 * half, stat = (int64_t)h * a.q_rows + s.q0 + token;
   Frag<T> qf[D / 16], df[D / 16];
@@ -502,11 +586,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_bwd_q_k(
     if (((col >> 2) & 1) != half) delta = other;
   }
   const float lse2 = a.lse[stat] * kLog2e;
-  if (row < rows && half == 0) reinterpret_cast<float2*>(a.delta)[((int64_t)head * a.q_rows + s.q0) * group + row] = make_float2(lse2, delta);
+  if (row < rows && half == 0 && (RB > 32 || wave == 0)) reinterpret_cast<float2*>(a.delta)[((int64_t)head * a.q_rows + s.q0) * group + row] = make_float2(lse2, delta);
   const int lo = key_begin(a, s, token), hi = row < rows ? key_end(a, s, token) : 0;
-  const int t_first = r0 / group, t_last = (min(r0 + RB, rows) - 1) / group;
+  const int t_first = a.group.of(r0), t_last = a.group.of(min(r0 + RB, rows) - 1);
   const int j_lo = key_begin(a, s, t_first), j_hi = key_end(a, s, t_last);
-  const int wr = r0 + 32 * wave, wt0 = min(wr, rows - 1) / group, wt1 = (min(wr + 32, rows) - 1) / group;
+  const int wt0 = a.group.of(min(wr, rows - 1)), wt1 = a.group.of(min(wr + 32, rows) - 1);
   const int w_lo = key_begin(a, s, wt1), w_hi = key_end(a, s, wt0), any_lo = key_begin(a, s, wt0), any_hi = wr < rows ? key_end(a, s, wt1) : 0;
 
   const T* kp = static_cast<const T*>(a.k) + s.k0 * a.ld_k + head * D;
@@ -529,11 +613,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_bwd_q_k(
       vs.load(vp, a.ld_v, j0 + KT, s.kn);
     }
 #pragma unroll
-    for (int t = 0; t < KT / 32; ++t) {
-      const int j = j0 + 32 * t;
+    for (int t = 0; t < NS; ++t) {
+      const int at = RB == 32 ? 32 * wave : 32 * t, j = j0 + at;
       if (j >= any_hi || j + 32 <= any_lo) continue;
-      f32x16_t p = rows_times<T, D>(Ks, 32 * t, lane, qf);
-      f32x16_t dp = rows_times<T, D>(Vs, 32 * t, lane, df);
+      f32x16_t p = rows_times<T, D>(Ks, at, lane, [&](int kk) { return qf[kk]; });
+      f32x16_t dp = rows_times<T, D>(Vs, at, lane, [&](int kk) { return df[kk]; });
 #pragma unroll
       for (int r = 0; r < 16; ++r) dp[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, -lse2)) * (dp[r] - delta);
       if (j < w_lo || j + 32 > w_hi) {
@@ -543,41 +627,63 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void seq_bwd_q_k(
           if (key < lo || key >= hi) dp[r] = 0.f;
         }
       }
-      add_rows<T, D>(dq, Ks, 32 * t, lane, dp);
+      add_rows<T, D>(dq, Ks, at, lane, dp);
     }
     __syncthreads();
   }
-  if (row < rows) store_column<T, D>(static_cast<T*>(a.dq) + (s.q0 + token) * a.ld_q + h * D, dq, a.scale, half);
+  if constexpr (RB == 32) {  // the wavefronts' sums meet in the first one
+    float* x = reinterpret_cast<float*>(tiles) + lane;
+    if (wave > 0) {
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[(wave - 1) * 32 * D + (e * 16 + r) * 64] = dq[e][r];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll 1
+    for (int w = 1; w < kWaves; ++w)
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dq[e][r] += x[(w - 1) * 32 * D + (e * 16 + r) * 64];
+  }
+  if constexpr (RB == 32) wave_fence();  // the sums have been read
+  store_rows<T, D>(tiles + (RB == 32 ? 0 : wave * 32 * S), dq, a.scale, lane, [&](int r) -> T* {
+    const int at = wr + r, t = a.group.of(at);
+    return at < rows ? static_cast<T*>(a.dq) + (s.q0 + t) * a.ld_q + (head * group + at - t * group) * D : nullptr;
+  });
 }
 
-// Gradients of keys and values: 128 keys a block, 32 a wavefront, the queries of all heads of the group in tiles that the wavefronts
-// share.  Both gradients, both operands and two tiles of scores are some 230 registers a lane at head dimension 128, which allows two
-// wavefronts a SIMD.  They are two that own the same keys and take every other tile of rows, and meet in LDS at the end: with
-// other keys for the second one there would be half as many blocks, each twice as long, and under a causal mask the block of the
-// first keys would outlast the others by half of the kernel's time (2 x 4096 tokens, 32 heads on 8: 1230 us).
-// Tiles are written to LDS one step ahead, so that there is one barrier a step.  (fp32 fills the registers with one wavefront.)
-template <class T>
-constexpr int kRowParts = sizeof(T) == 2 ? 2 : 1;
+// Gradients of keys and values: RB keys a block, 32 a wavefront, the queries of all heads of the group in tiles of rows.  P wavefronts own
+// the same keys, take every P-th tile, and meet in LDS at the end.  Both gradients, both operands and two tiles of scores are some 230
+// registers a lane at head dimension 128, which allows two wavefronts a SIMD.
+//   <128, 2>  few blocks a compute unit: the two wavefronts of a SIMD share their keys.  With other keys for the second one there would be
+//             half as many blocks, each twice as long, and under a causal mask the block of the first keys would outlast the others by half
+//             of the kernel's time (2 x 4096 tokens, 32 heads on 8, 128 wide: 690 against 1230 us).
+//   <128, 1>  many blocks, in which starts and ends of some hide behind others.
+//   <32, 4>   fewer blocks than compute units.
+// Tiles are written to LDS one step ahead, so that there is one barrier a step.
 // fragments of the values (of D / 16) that lie in LDS, a thread's own, since the registers do not hold them
 template <class T, int D>
-constexpr int kValuesInLds = sizeof(T) == 2 && D == 128 ? 8 : 0;
+constexpr int kValuesInLds = sizeof(T) == 2 ? D == 128 ? 8 : D == 64 ? 4 : 0 : 0;
 // rows of a wavefront's tile
 template <class T, int D>
 constexpr int kQueryTile = sizeof(T) == 2 && D == 32 ? 64 : 32;
 
-template <class T, int D>
-__global__ __launch_bounds__(kThreads* kRowParts<T>, kRowParts<T>) void seq_bwd_k_k(SeqAttn a) {
-  constexpr int P = kRowParts<T>, NT = kThreads * P, RB = 128, WT = kQueryTile<T, D>, QT = WT * P, S = kStride<T, D>;
-  constexpr int kTileBytes = 4 * QT * S * (int)sizeof(T), kMergeBytes = P > 1 ? RB * D * 4 : 0;
-  __shared__ __attribute__((aligned(16))) char tiles[kTileBytes > kMergeBytes ? kTileBytes : kMergeBytes];
+template <class T, int D, int RB, int P>
+__global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64) ? 1 : D == 128 || P > 1 ? 2 : 3) void seq_bwd_k_k(SeqAttn a) {
+  constexpr int NT = 2 * RB * P, WT = kQueryTile<T, D>, QT = WT * P, S = kStride<T, D>;
+  constexpr int kTileBytes = 4 * QT * S * (int)sizeof(T), kMergeBytes = (P - 1) * RB * D * 4;
+  __shared__ __attribute__((aligned(256))) char tiles[kTileBytes > kMergeBytes ? kTileBytes : kMergeBytes];
   const auto Qs = [&](int buf) { return reinterpret_cast<T*>(tiles) + buf * QT * S; };
   const auto Cs = [&](int buf) { return reinterpret_cast<T*>(tiles) + (2 + buf) * QT * S; };
-  constexpr int VL = kValuesInLds<T, D>, VR = D / 16 - VL;
+  constexpr int VL = RB == 32 ? 0 : kValuesInLds<T, D>, VR = D / 16 - VL;
   __shared__ Frag<T> v_lds[VL > 0 ? VL : 1][VL > 0 ? NT : 1];
   __shared__ __attribute__((aligned(16))) float stats[2][2][QT];  // log-sum-exp times log2(e), delta
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = w % kWaves, part = w / kWaves;
-  const int group = a.hq / a.hk, head = blockIdx.x % a.hk;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = w % (RB / 32), part = w / (RB / 32);
+  const int group = a.group.d, head = blockIdx.x % a.hk;
   const int slot = (int)(blockIdx.x / a.hk);  // the first keys are seen by the most queries
   const Seq s = find_sequence<true>(a, 1, RB, slot);
   const int j0 = s.tile * RB;
@@ -614,7 +720,7 @@ __global__ __launch_bounds__(kThreads* kRowParts<T>, kRowParts<T>) void seq_bwd_
     dv[e] = zero16();
   }
   const float c = a.scale * kLog2e;
-  const int quotient = QT / group, rest = QT - quotient * group;
+  const int quotient = a.group.of(QT), rest = QT - quotient * group;
   QueryRows<T, D, QT, NT> qr;
   float2 stat = make_float2(0.f, 0.f);
   const auto load = [&](int r) {
@@ -629,7 +735,7 @@ __global__ __launch_bounds__(kThreads* kRowParts<T>, kRowParts<T>) void seq_bwd_
     }
   };
   if (r_lo < r_hi) {
-    qr.start(group, r_lo);
+    qr.start(a.group, r_lo);
     load(r_lo);
     store(0);
     if (r_lo + QT < r_hi) load(r_lo + QT);
@@ -644,15 +750,8 @@ __global__ __launch_bounds__(kThreads* kRowParts<T>, kRowParts<T>) void seq_bwd_
     for (int t = 0; t < WT / 32; ++t) {
       const int at_t = part * WT + 32 * t, rt = r + at_t;
       if (rt >= any_hi || rt + 32 <= any_lo) continue;
-      f32x16_t p = rows_times<T, D>(Qs(buf), at_t, lane, kf);
-      f32x16_t dp = zero16();
-      {
-        const T* cr = Cs(buf) + (at_t + col) * S + 8 * half;
-#pragma unroll
-        for (int kk = 0; kk < VR; ++kk) dp = mma(load8(cr + 16 * kk), vf[kk], dp);
-#pragma unroll
-        for (int kk = VR; kk < D / 16; ++kk) dp = mma(load8(cr + 16 * kk), v_lds[kk - VR][threadIdx.x], dp);
-      }
+      f32x16_t p = rows_times<T, D>(Qs(buf), at_t, lane, [&](int kk) { return kf[kk]; });
+      f32x16_t dp = rows_times<T, D>(Cs(buf), at_t, lane, [&](int kk) { return kk < VR ? vf[kk < VR ? kk : 0] : v_lds[kk < VR ? 0 : kk - VR][VL > 0 ? threadIdx.x : 0]; });
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float4 ls = *reinterpret_cast<const float4*>(&stats[buf][0][at_t + 8 * i + 4 * half]);
@@ -679,7 +778,7 @@ __global__ __launch_bounds__(kThreads* kRowParts<T>, kRowParts<T>) void seq_bwd_
     }
     __syncthreads();
   }
-  if constexpr (P > 1) {  // the second part's sums are added to the first's, one gradient after the other
+  if constexpr (P > 1) {  // the other parts' sums are added to the first's, one gradient after the other
     float* x = reinterpret_cast<float*>(tiles) + wave * 32 * D + lane;
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
@@ -688,33 +787,44 @@ __global__ __launch_bounds__(kThreads* kRowParts<T>, kRowParts<T>) void seq_bwd_
 #pragma unroll
         for (int e = 0; e < D / 32; ++e)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) x[(e * 16 + i) * 64] = acc[e][i];
+          for (int i = 0; i < 16; ++i) x[(part - 1) * RB * D + (e * 16 + i) * 64] = acc[e][i];
       }
       __syncthreads();
       if (part == 0) {
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e)
+        for (int o = 0; o < P - 1; ++o)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[e][i] += x[(e * 16 + i) * 64];
+          for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[e][i] += x[o * RB * D + (e * 16 + i) * 64];
       }
       if (g == 0) __syncthreads();
     }
     if (part > 0) return;
   }
-  if (key < s.kn) {
-    store_column<T, D>(static_cast<T*>(a.dk) + (s.k0 + key) * a.ld_k + head * D, dk, a.scale, half);
-    store_column<T, D>(static_cast<T*>(a.dv) + (s.k0 + key) * a.ld_v + head * D, dv, 1.f, half);
-  }
+  if constexpr (P > 1) wave_fence();  // the sums have been read; their place is this wavefront's own
+  T* scratch = reinterpret_cast<T*>(tiles) + wave * (P > 1 ? 32 * D * 4 / (int)sizeof(T) : 32 * S);
+  static_assert(P > 1 ? 32 * D * 4 >= 32 * S * (int)sizeof(T) || sizeof(T) == 4 : kTileBytes >= RB * S * (int)sizeof(T) || sizeof(T) == 4, "rows are put together where the tiles were");
+  const auto rows_of = [&](void* base, int64_t ld) {
+    return [=](int r) -> T* { return j0 + 32 * wave + r < s.kn ? static_cast<T*>(base) + (s.k0 + j0 + 32 * wave + r) * ld + head * D : nullptr; };
+  };
+  store_rows<T, D>(scratch, dk, a.scale, lane, rows_of(a.dk, a.ld_k));
+  store_rows<T, D>(scratch, dv, 1.f, lane, rows_of(a.dv, a.ld_v));
 }
 
 // ---- launches ----------------------------------------------------------------
-// few queries a sequence, on the average (their number is not known on the host): blocks of 32 rows
-bool few_rows(const SeqAttn& a) { return a.q_rows * (a.hq / a.hk) <= (int64_t)32 * a.batch; }
+constexpr int kUnits = 256;  // compute units
+// Blocks of 128 rows while there is one for each compute unit.  Below that, and where a sequence has on the average fewer rows than
+// half a block (the lengths are not known on the host), blocks of 32 rows, whose wavefronts share out the keys.
+bool few_rows(const SeqAttn& a) {
+  const int64_t group = a.hq / a.hk;
+  return slots(a.q_rows, a.batch, (int)group, 128) * a.hk < kUnits || a.q_rows * group <= (int64_t)64 * a.batch;
+}
 // keys are shared out among blocks while there are fewer than four blocks a compute unit, each keeping two tiles
 int splits(const SeqAttn& a) {
   if (!few_rows(a) || a.q_rows == 0) return 1;
   const int64_t blocks = slots(a.q_rows, a.batch, a.hq / a.hk, 32) * a.hk, keys = (a.k_rows + a.batch - 1) / a.batch;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({1024 / blocks, keys / 256, 32}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({4 * kUnits / blocks, keys / 256, 32}));
 }
 
 template <class T, int D>
@@ -730,8 +840,21 @@ void forward(const SeqAttn& a, hipStream_t st) {
 }
 template <class T, int D>
 void backward(const SeqAttn& a, hipStream_t st) {
-  if (a.q_rows) seq_bwd_q_k<T, D><<<(unsigned)(slots(a.q_rows, a.batch, a.hq / a.hk, 128) * a.hk), kThreads, 0, st>>>(a);
-  if (a.k_rows) seq_bwd_k_k<T, D><<<(unsigned)(slots(a.k_rows, a.batch, 1, 128) * a.hk), kThreads * kRowParts<T>, 0, st>>>(a);
+  const int group = a.hq / a.hk;
+  if (a.q_rows) {
+    if (few_rows(a)) seq_bwd_q_k<T, D, 32><<<(unsigned)(slots(a.q_rows, a.batch, group, 32) * a.hk), kThreads, 0, st>>>(a);
+    else seq_bwd_q_k<T, D, 128><<<(unsigned)(slots(a.q_rows, a.batch, group, 128) * a.hk), kThreads, 0, st>>>(a);
+  }
+  if (!a.k_rows) return;
+  const int64_t n = slots(a.k_rows, a.batch, 1, 128) * a.hk;
+  constexpr bool kSmall = sizeof(T) == 2 || D < 128;  // what LDS and registers hold
+  if (kSmall && n < kUnits) {
+    if constexpr (kSmall) seq_bwd_k_k<T, D, 32, 4><<<(unsigned)(slots(a.k_rows, a.batch, 1, 32) * a.hk), 256, 0, st>>>(a);
+  } else if (sizeof(T) == 2 && (D == 128 || n < 3 * kUnits)) {
+    if constexpr (sizeof(T) == 2) seq_bwd_k_k<T, D, 128, 2><<<(unsigned)n, 512, 0, st>>>(a);
+  } else {
+    seq_bwd_k_k<T, D, 128, 1><<<(unsigned)n, 256, 0, st>>>(a);
+  }
 }
 
 #define MREM_SEQ_DISPATCH(f)                                    \
