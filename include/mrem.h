@@ -345,7 +345,7 @@ mrem_status mrem_rotary_backward(const void* dy, void* dx, int32_t dtype, int64_
  * finite reaches only queries and keys that see it or lie in the same tile of up to 128.
  * head_dim 32, 64 or 128; q_heads a multiple of kv_heads; q_rows * (q_heads / kv_heads) and k_rows < 2^31 - 2^20, and each of
  * them / 32, plus batch, times kv_heads < 2^24; strides
- * multiples of 16 bytes and at least heads * head_dim; pointers 16-byte aligned.  Outputs may not overlap inputs.
+ * multiples of 16 bytes, at least heads * head_dim and at most 2^21; pointers 16-byte aligned.  Outputs may not overlap inputs.
  * workspace: mrem_attention_workspace_bytes(cfg, backward) bytes (0: may be NULL), not shared by calls that overlap in time; the
  * contents carry nothing from call to call.
  */

@@ -1490,9 +1490,9 @@ static mrem_status attention_shape(const char* who, const mrem_attention_config*
   // a block of 256 threads takes 32 rows or more of a key head: a launch has fewer than 2^32 threads
   if ((c.q_rows * group / 32 + c.batch) * c.kv_heads >= (int64_t)1 << 24 || (c.k_rows / 32 + c.batch) * c.kv_heads >= (int64_t)1 << 24)
     return bad(MREM_ESHAPE, "too many rows times heads");
-  const int64_t piece = 16 / (int64_t)dt_size(dt_of(c.dtype)), limit = (int64_t)1 << 40;
+  const int64_t piece = 16 / (int64_t)dt_size(dt_of(c.dtype)), limit = (int64_t)1 << 21;
   for (int64_t ld : {c.ld_q, c.ld_k, c.ld_v, c.ld_out})
-    if (ld % piece || ld > limit) return bad(MREM_ESHAPE, "strides must be multiples of 16 bytes");
+    if (ld % piece || ld > limit) return bad(MREM_ESHAPE, "strides must be multiples of 16 bytes, <= 2^21 elements");
   if (c.ld_q < (int64_t)c.q_heads * c.head_dim || c.ld_out < (int64_t)c.q_heads * c.head_dim || c.ld_k < (int64_t)c.kv_heads * c.head_dim ||
       c.ld_v < (int64_t)c.kv_heads * c.head_dim)
     return bad(MREM_ESHAPE, "rows overlap: stride below heads * head_dim");

@@ -116,57 +116,95 @@ __device__ __forceinline__ Frag<T> from_acc(const f32x16_t& a, int s) {
   for (int i = 0; i < 8; ++i) f.v[i] = static_cast<T>(a[8 * s + i]);
   return f;
 }
+// Fragments of a tile, in the order in which a product takes them: along its rows (32 of them, piece by piece), or down its columns
+// (of 32 rows, 32 columns for each e, row r of accumulator register order: 16 s + 4 (lane / 32) + 0..3 and 8 more).
+template <class T, int D>
+struct AlongRows {
+  static constexpr int kCount = D / 16;
+  const T* p;
+  unsigned a = 0;
+  __device__ __forceinline__ AlongRows(const T* tile, int row0, int lane) {
+    const int at = lds_at<T, D>(row0 + (lane & 31), 8 * (lane >> 5));
+    p = tile + at;
+    if constexpr (sizeof(T) == 2) a = lane_address(tile, at);
+  }
+  __device__ __forceinline__ Frag<T> operator()(int kk) const {
+    if constexpr (sizeof(T) == 2) return Frag<T>{read8(a ^ (32 * kk))};
+    else return load8(p + 16 * kk);
+  }
+};
+template <class T, int D>
+struct DownColumns {
+  static constexpr int kCount = D / 16;  // s, e
+  const T* p;
+  unsigned a = 0;
+  __device__ __forceinline__ DownColumns(const T* tile, int row0, int lane) {
+    if constexpr (sizeof(T) == 2) {
+      // the transposing read: in a group of 16 lanes, lane s names columns 4 (s % 4) .. + 3 of row s / 4 and receives column s of the four rows
+      const int g = lane >> 4, s16 = lane & 15;
+      a = lane_address(tile, lds_at<T, D>(row0 + 4 * (lane >> 5) + (s16 >> 2), 16 * (g & 1) + 4 * (s16 & 3)));
+    } else {
+      p = tile + (row0 + 4 * (lane >> 5)) * kStride<T, D> + (lane & 31);
+    }
+  }
+  __device__ __forceinline__ Frag<T> operator()(int n) const {
+    const int s = n / (D / 32), e = n % (D / 32);
+    if constexpr (sizeof(T) == 2) {
+      union { bf16x8_t v; s16x4_t h[2]; } u;
+      u.h[0] = read_tr((a ^ (64 * e)) + 32 * s * D);
+      u.h[1] = read_tr((a ^ (64 * e) ^ 32) + (32 * s + 16) * D);  // 8 rows on: piece_of differs in its bit 1
+      return Frag<T>{u.v};
+    } else {
+      Frag<T> u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        u.v[i] = p[(16 * s + i) * kStride<T, D> + 32 * e];
+        u.v[4 + i] = p[(16 * s + 8 + i) * kStride<T, D> + 32 * e];
+      }
+      return u;
+    }
+  }
+};
+// Fragments on their way to the matrix instructions.  An LDS read takes as long as four of these, so the fourth next fragment is read behind each
+// instruction; left to itself the compiler reads one ahead, and the instructions wait for two thirds of the time.
+template <class T>
+struct Ahead {
+  static constexpr int kDepth = sizeof(T) == 2 ? 4 : 1;
+  Frag<T> f[kDepth];
+  template <class L>
+  __device__ __forceinline__ void start(const L& read) {
+#pragma unroll
+    for (int i = 0; i < kDepth; ++i) f[i] = read(i);
+  }
+  // products 0 .. N - 1; `started`: the first fragments are being read already
+  template <int N, class L, class M>
+  __device__ __forceinline__ void run(const L& read, const M& multiply) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      multiply(n, f[n % kDepth]);
+      if (n + kDepth < N) f[n % kDepth] = read(n + kDepth);
+      if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
 // 32 x 32 tile: LDS rows [row0, row0 + 32) times the 32 rows held as fragments b(kk), 16 columns each
 template <class T, int D, class B>
 __device__ __forceinline__ f32x16_t rows_times(const T* tile, int row0, int lane, B b) {
   f32x16_t acc = zero16();
-  const int row = row0 + (lane & 31), at = lds_at<T, D>(row, 8 * (lane >> 5));
-  if constexpr (sizeof(T) == 2) {
-    const unsigned a = lane_address(tile, at);
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) acc = mma(Frag<T>{read8(a ^ (32 * kk))}, b(kk), acc);
-  } else {
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) acc = mma(load8(tile + at + 16 * kk), b(kk), acc);
-  }
+  const AlongRows<T, D> rows(tile, row0, lane);
+  Ahead<T> ahead;
+  ahead.start(rows);
+  ahead.template run<D / 16>(rows, [&](int kk, const Frag<T>& f) { acc = mma(f, b(kk), acc); });
   return acc;
 }
-// acc[e][.] += sum over the tile's 32 rows of tile[row][e] w[row], w in accumulator order: the tile's fragments run down its rows, column
-// 32 e + lane % 32, rows 16 s + 4 (lane / 32) + 0..3 and 8 more
+// acc[e][.] += sum over the tile's 32 rows of tile[row][e] w[row], w in accumulator order
 template <class T, int D>
 __device__ __forceinline__ void add_rows(f32x16_t (&acc)[D / 32], const T* tile, int row0, int lane, const f32x16_t& w) {
-  if constexpr (sizeof(T) == 2) {
-    // the transposing read: in a group of 16 lanes, lane s names columns 4 (s % 4) .. + 3 of row s / 4 and receives column s of the four rows
-    const int g = lane >> 4, s16 = lane & 15, row = row0 + 4 * (lane >> 5) + (s16 >> 2), col = 16 * (g & 1) + 4 * (s16 & 3);
-    const unsigned a = lane_address(tile, lds_at<T, D>(row, col));
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const Frag<T> f = from_acc<T>(w, s);
-#pragma unroll
-      for (int e = 0; e < D / 32; ++e) {
-        union { bf16x8_t v; s16x4_t h[2]; } u;
-        u.h[0] = read_tr((a ^ (64 * e)) + 32 * s * D);
-        u.h[1] = read_tr((a ^ (64 * e) ^ 32) + (32 * s + 16) * D);  // 8 rows on: piece_of differs in its bit 1
-        acc[e] = mma(Frag<T>{u.v}, f, acc[e]);
-      }
-    }
-  } else {
-    const T* p = tile + (row0 + 4 * (lane >> 5)) * kStride<T, D> + (lane & 31);
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const Frag<T> f = from_acc<T>(w, s);
-#pragma unroll
-      for (int e = 0; e < D / 32; ++e) {
-        Frag<T> u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          u.v[i] = p[(16 * s + i) * kStride<T, D> + 32 * e];
-          u.v[4 + i] = p[(16 * s + 8 + i) * kStride<T, D> + 32 * e];
-        }
-        acc[e] = mma(u, f, acc[e]);
-      }
-    }
-  }
+  const DownColumns<T, D> columns(tile, row0, lane);
+  Ahead<T> ahead;
+  ahead.start(columns);
+  const Frag<T> f[2] = {from_acc<T>(w, 0), from_acc<T>(w, 1)};
+  ahead.template run<D / 16>(columns, [&](int n, const Frag<T>& u) { acc[n % (D / 32)] = mma(u, f[n / (D / 32)], acc[n % (D / 32)]); });
 }
 // LDS accesses of a wavefront are carried out in order: nothing is to be moved across, that is all
 __device__ __forceinline__ void wave_fence() { asm volatile("" ::: "memory"); }
@@ -233,62 +271,70 @@ __device__ __forceinline__ int key_begin(const SeqAttn& a, const Seq& s, int i) 
 }
 
 // ---- tiles on their way to LDS -----------------------------------------------
-// rows [j0, j0 + ROWS) of a matrix of n rows; rows behind it are zero
+// Tiles are read through a buffer descriptor that ends where the tile's rows do: a thread's place in it is a 32-bit offset that stays the
+// same from tile to tile, what lies behind the end is read as zero by the load itself, and the address is the scalar unit's.  (With 64-bit
+// addresses and tests a tile cost a lane 105 vector instructions, half as many as its softmax.)  Strides are up to 2^21 elements.
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+template <class T>
+__device__ __forceinline__ rsrc_t window(const T* base, int64_t elements) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, (int)(elements * (int)sizeof(T)), 0x00027000);
+}
+// (the whole offset in the vector part, which is what the end is compared with)
+__device__ __forceinline__ u32x4_t read16(rsrc_t r, unsigned offset) { return __builtin_amdgcn_raw_buffer_load_b128(r, (int)offset, 0, 0); }
+
+// rows [j0, j0 + ROWS) of a matrix of n > j0 rows whose first element is at src; rows behind it are zero
 template <class T, int D, int ROWS>
 struct Stage {
-  static constexpr int kPiece = 16 / sizeof(T), kRowPieces = D / kPiece, kAll = ROWS * kRowPieces, kN = (kAll + kThreads - 1) / kThreads;
-  static_assert(kAll % kThreads == 0 || kN == 1, "whole pieces a thread, or one for some");
+  static constexpr int kPiece = 16 / sizeof(T), kRowPieces = D / kPiece, kN = ROWS * kRowPieces / kThreads, kApart = kThreads / kRowPieces;
+  static_assert(ROWS * kRowPieces % kThreads == 0, "whole pieces a thread");
   u32x4_t v[kN];
   __device__ __forceinline__ void load(const T* __restrict__ src, int64_t ld, int j0, int n) {
+    const rsrc_t tile = window(src + j0 * ld, (min(ROWS, n - j0) - 1) * ld + D);
+    const unsigned bytes = (unsigned)ld * (unsigned)sizeof(T), offset = threadIdx.x / kRowPieces * bytes + threadIdx.x % kRowPieces * 16;
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const int q = threadIdx.x + i * kThreads, row = min(j0 + q / kRowPieces, n - 1);
-      v[i] = *reinterpret_cast<const u32x4_t*>(src + row * ld + q % kRowPieces * kPiece);
-    }
+    for (int i = 0; i < kN; ++i) v[i] = read16(tile, offset + i * kApart * bytes);
   }
-  __device__ __forceinline__ void store(T* dst, int j0, int n) const {
+  __device__ __forceinline__ void store(T* dst) const {
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const int q = threadIdx.x + i * kThreads, row = q / kRowPieces;
-      if (kAll % kThreads == 0 || q < kAll) *reinterpret_cast<u32x4_t*>(dst + lds_at<T, D>(row, q % kRowPieces * kPiece)) = j0 + row < n ? v[i] : u32x4_t{0u, 0u, 0u, 0u};
-    }
+    for (int i = 0; i < kN; ++i) *reinterpret_cast<u32x4_t*>(dst + lds_at<T, D>(threadIdx.x / kRowPieces + i * kApart, threadIdx.x % kRowPieces * kPiece)) = v[i];
   }
 };
-// Rows of the packed axis, (token r / group, head r % group), tile after tile: a thread's rows are kThreads / pieces apart and move on
-// by a tile's rows, so their places advance by a quotient and a remainder that are divided once.
+// Rows of the packed axis, (token r / group, head r % group), tile after tile, of two tensors: a thread's rows are kThreads / pieces apart and
+// move on by a tile's rows, so their places advance by a quotient and a remainder that are divided once.
 template <class T, int D, int ROWS, int THREADS>
 struct QueryRows {
   static constexpr int kPiece = 16 / sizeof(T), kRowPieces = D / kPiece, kN = ROWS * kRowPieces / THREADS, kApart = THREADS / kRowPieces;
   static_assert(ROWS * kRowPieces % THREADS == 0, "whole pieces a thread");
-  int token[kN];
-  int head[kN];
+  int token[kN], head[kN], first;
   u32x4_t q[kN], c[kN];
   __device__ __forceinline__ void start(const Divisor& group, int r0) {
+    first = group.of(r0);
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int row = r0 + threadIdx.x / kRowPieces + i * kApart, t = group.of(row);
-      token[i] = t;
+      token[i] = t - first;
       head[i] = row - t * group.d;
     }
   }
-  // rows r0 + ... of the two tensors (zeros behind n); then the next tile's places
-  __device__ __forceinline__ void load(const T* __restrict__ qs, int64_t ld_q, const T* __restrict__ cs, int64_t ld_c, int r0, int n, int group, int quotient, int rest) {
-    const int at = threadIdx.x % kRowPieces * kPiece;
+  // rows r0 + ... < n (zeros behind them), `first` the token of row r0; then the next tile's places
+  __device__ __forceinline__ void load(const T* __restrict__ qs, int64_t ld_q, const T* __restrict__ cs, int64_t ld_c, int r0, int n, const Divisor& group) {
+    const int tokens = min(ROWS, group.of(n - 1) - first + 1);  // that the tile's rows are of, or more
+    const rsrc_t qw = window(qs + first * ld_q, (tokens - 1) * ld_q + group.d * D), cw = window(cs + first * ld_c, (tokens - 1) * ld_c + group.d * D);
+    const unsigned bytes_q = (unsigned)ld_q * (unsigned)sizeof(T), bytes_c = (unsigned)ld_c * (unsigned)sizeof(T);
+    const int next = group.of(r0 + ROWS), quotient = group.of(ROWS), rest = ROWS - quotient * group.d;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      q[i] = c[i] = u32x4_t{0u, 0u, 0u, 0u};
-      if (r0 + (int)(threadIdx.x / kRowPieces) + i * kApart < n) {
-        const int col = head[i] * D + at;
-        q[i] = *reinterpret_cast<const u32x4_t*>(qs + (int64_t)token[i] * ld_q + col);
-        c[i] = *reinterpret_cast<const u32x4_t*>(cs + (int64_t)token[i] * ld_c + col);
-      }
+      const unsigned col = head[i] * (D * (int)sizeof(T)) + threadIdx.x % kRowPieces * 16;
+      q[i] = read16(qw, __umul24(token[i], bytes_q) + col);
+      c[i] = read16(cw, __umul24(token[i], bytes_c) + col);
+      token[i] += quotient - (next - first);
       head[i] += rest;
-      token[i] += quotient;
-      if (head[i] >= group) {
-        head[i] -= group;
+      if (head[i] >= group.d) {
+        head[i] -= group.d;
         token[i] += 1;
       }
     }
+    first = next;
   }
   __device__ __forceinline__ void store(T* qs, T* cs) const {
 #pragma unroll
@@ -351,8 +397,7 @@ __global__ __launch_bounds__(kThreads, (kForwardWaves<T, D, RB>)) void seq_fwd_k
   constexpr int kTileBytes = 2 * KT * S * (int)sizeof(T), kMergeBytes = RB == 32 ? 32 * D * 4 * (kWaves - 1) : 0;
   __shared__ __attribute__((aligned(256))) char lds[kTileBytes > kMergeBytes ? kTileBytes : kMergeBytes];
   __shared__ float merge_m[kWaves][32], merge_l[kWaves][32];
-  T* Ks = reinterpret_cast<T*>(lds);
-  T* Vs = Ks + KT * S;
+  T *const Ks = reinterpret_cast<T*>(lds), *const Vs = Ks + KT * S;
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = a.group.d;
   const int head = blockIdx.x % a.hk, split = blockIdx.y;
@@ -387,18 +432,16 @@ __global__ __launch_bounds__(kThreads, (kForwardWaves<T, D, RB>)) void seq_fwd_k
   float m = -INFINITY, l = 0.f;  // what exponentials are taken against (a score, without scale), this lane's part of their sum
   const float c = a.scale * kLog2e;
   Stage<T, D, KT> ks, vs;
-  if (j_lo < j_hi) {
-    ks.load(kp, a.ld_k, j_lo, s.kn);
-    vs.load(vp, a.ld_v, j_lo, s.kn);
-  }
+  const auto load = [&](int j) {
+    ks.load(kp, a.ld_k, j, s.kn);
+    vs.load(vp, a.ld_v, j, s.kn);
+  };
+  if (j_lo < j_hi) load(j_lo);
   for (int j0 = j_lo; j0 < j_hi; j0 += KT) {
-    ks.store(Ks, j0, s.kn);
-    vs.store(Vs, j0, s.kn);
+    ks.store(Ks);
+    vs.store(Vs);
     __syncthreads();
-    if (j0 + KT < j_hi) {
-      ks.load(kp, a.ld_k, j0 + KT, s.kn);
-      vs.load(vp, a.ld_v, j0 + KT, s.kn);
-    }
+    if (j0 + KT < j_hi) load(j0 + KT);
     const int base = RB == 32 ? 32 * wave : 0;
     if (j0 + base < any_hi && j0 + base + 32 * NS > any_lo) {
       f32x16_t p[NS];
@@ -559,7 +602,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
   constexpr int KT = kKeyTile<T, RB>, NS = RB == 32 ? 1 : KT / 32, S = kStride<T, D>;
   static_assert(2 * KT * S * (int)sizeof(T) >= (RB == 32 ? 32 * D * 4 * (kWaves - 1) : 0), "the sums meet where the tiles were");
   __shared__ __attribute__((aligned(256))) T tiles[2 * KT * S];
-  T *Ks = tiles, *Vs = tiles + KT * S;
+  T *const Ks = tiles, *const Vs = tiles + KT * S;
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = a.group.d, head = blockIdx.x % a.hk;
   const int slot = (int)(gridDim.x / a.hk - 1 - blockIdx.x / a.hk);
@@ -600,18 +643,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
   for (int e = 0; e < D / 32; ++e) dq[e] = zero16();
   const float c = a.scale * kLog2e;
   Stage<T, D, KT> ks, vs;
-  if (j_lo < j_hi) {
-    ks.load(kp, a.ld_k, j_lo, s.kn);
-    vs.load(vp, a.ld_v, j_lo, s.kn);
-  }
+  const auto load = [&](int j) {
+    ks.load(kp, a.ld_k, j, s.kn);
+    vs.load(vp, a.ld_v, j, s.kn);
+  };
+  if (j_lo < j_hi) load(j_lo);
   for (int j0 = j_lo; j0 < j_hi; j0 += KT) {
-    ks.store(Ks, j0, s.kn);
-    vs.store(Vs, j0, s.kn);
+    ks.store(Ks);
+    vs.store(Vs);
     __syncthreads();
-    if (j0 + KT < j_hi) {
-      ks.load(kp, a.ld_k, j0 + KT, s.kn);
-      vs.load(vp, a.ld_v, j0 + KT, s.kn);
-    }
+    if (j0 + KT < j_hi) load(j0 + KT);
 #pragma unroll
     for (int t = 0; t < NS; ++t) {
       const int at = RB == 32 ? 32 * wave : 32 * t, j = j0 + at;
@@ -720,11 +761,10 @@ __global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64)
     dv[e] = zero16();
   }
   const float c = a.scale * kLog2e;
-  const int quotient = a.group.of(QT), rest = QT - quotient * group;
   QueryRows<T, D, QT, NT> qr;
   float2 stat = make_float2(0.f, 0.f);
   const auto load = [&](int r) {
-    qr.load(qp, a.ld_q, cp, a.ld_o, r, rows, group, quotient, rest);
+    qr.load(qp, a.ld_q, cp, a.ld_o, r, rows, a.group);
     if ((int)threadIdx.x < QT) stat = sp[min(r + (int)threadIdx.x, rows - 1)];
   };
   const auto store = [&](int buf) {

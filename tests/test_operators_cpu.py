@@ -63,7 +63,7 @@ def test_attention_refusals(B):
 
     shapes = [dict(dtype=2), dict(head_dim=96), dict(head_dim=0), dict(kv_heads=0), dict(kv_heads=3), dict(q_heads=0), dict(batch=0), dict(causal=2), dict(window=-1),
               dict(causal=0, window=5), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(q_rows=-1), dict(q_rows=1 << 31), dict(k_rows=1 << 31),
-              dict(q_rows=1 << 30), dict(ld_q=255), dict(ld_q=248), dict(ld_k=120), dict(ld_v=136 + 4), dict(ld_out=-256), dict(batch=1 << 20, kv_heads=64, q_heads=64, ld_q=4096, ld_k=4096, ld_v=4096, ld_out=4096)]
+              dict(q_rows=1 << 30), dict(ld_q=255), dict(ld_q=248), dict(ld_k=120), dict(ld_v=136 + 4), dict(ld_out=-256), dict(ld_v=(1 << 21) + 8), dict(batch=1 << 20, kv_heads=64, q_heads=64, ld_q=4096, ld_k=4096, ld_v=4096, ld_out=4096)]
     odd = ctypes.c_void_p(0x1008)
     for fn in (forward, backward):
         for change in shapes:
