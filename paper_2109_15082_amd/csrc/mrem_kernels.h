@@ -345,7 +345,7 @@ struct SeqAttn {
   const void *q, *k, *v, *dout;
   void *out, *dq, *dk, *dv;
   float* lse;    // [hq, q_rows]
-  float* delta;  // [hk, q_rows, hq / hk] pairs: lse times log2(e), out . d_out
+  float* delta;  // [hk, q_rows, hq / hk] pairs: -lse / scale (-inf for a row that sees nothing), out . d_out
   const int32_t *q_start, *k_start, *q_len, *k_len;
   float* part;  // partial results of keys shared out among blocks
   int splits;

@@ -166,45 +166,57 @@ struct DownColumns {
   }
 };
 // Fragments on their way to the matrix instructions.  An LDS read takes as long as four of these, so the fourth next fragment is read behind each
-// instruction; left to itself the compiler reads one ahead, and the instructions wait for two thirds of the time.
-template <class T>
+// instruction; left to itself the compiler reads one ahead, and the instructions wait for two thirds of the time.  `beside`: vector instructions
+// that the product does not need, a part of which goes behind each of its N instructions (which take as long as eight of them).
+struct Nothing {
+  __device__ __forceinline__ void operator()(int) const {}
+};
+template <class T, int DEPTH>
 struct Ahead {
-  static constexpr int kDepth = sizeof(T) == 2 ? 4 : 1;
+  static constexpr int kDepth = sizeof(T) == 2 ? DEPTH : 1;
   Frag<T> f[kDepth];
   template <class L>
   __device__ __forceinline__ void start(const L& read) {
 #pragma unroll
     for (int i = 0; i < kDepth; ++i) f[i] = read(i);
   }
-  // products 0 .. N - 1; `started`: the first fragments are being read already
-  template <int N, class L, class M>
-  __device__ __forceinline__ void run(const L& read, const M& multiply) {
+  template <int N, class L, class M, class B>
+  __device__ __forceinline__ void run(const L& read, const M& multiply, const B& beside) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       multiply(n, f[n % kDepth]);
       if (n + kDepth < N) f[n % kDepth] = read(n + kDepth);
+      beside(n);
       if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
     }
   }
 };
+// (with three wavefronts a SIMD instead of two, two fragments are enough, and all that the registers hold)
+template <int D>
+constexpr int kAhead = D == 128 ? 4 : 2;
+// element work of an accumulator's 16 registers in D / 16 parts
+template <int D, class F>
+__device__ __forceinline__ void part_of_16(int n, F f) {
+#pragma unroll
+  for (int r = 0; r < 256 / D; ++r) f(n * (256 / D) + r);
+}
 // 32 x 32 tile: LDS rows [row0, row0 + 32) times the 32 rows held as fragments b(kk), 16 columns each
-template <class T, int D, class B>
-__device__ __forceinline__ f32x16_t rows_times(const T* tile, int row0, int lane, B b) {
-  f32x16_t acc = zero16();
+template <class T, int D, class B, class F = Nothing>
+__device__ __forceinline__ f32x16_t rows_times(const T* tile, int row0, int lane, B b, F beside = F(), f32x16_t acc = zero16()) {
   const AlongRows<T, D> rows(tile, row0, lane);
-  Ahead<T> ahead;
+  Ahead<T, kAhead<D>> ahead;
   ahead.start(rows);
-  ahead.template run<D / 16>(rows, [&](int kk, const Frag<T>& f) { acc = mma(f, b(kk), acc); });
+  ahead.template run<D / 16>(rows, [&](int kk, const Frag<T>& f) { acc = mma(f, b(kk), acc); }, beside);
   return acc;
 }
 // acc[e][.] += sum over the tile's 32 rows of tile[row][e] w[row], w in accumulator order
-template <class T, int D>
-__device__ __forceinline__ void add_rows(f32x16_t (&acc)[D / 32], const T* tile, int row0, int lane, const f32x16_t& w) {
+template <class T, int D, class F = Nothing>
+__device__ __forceinline__ void add_rows(f32x16_t (&acc)[D / 32], const T* tile, int row0, int lane, const f32x16_t& w, F beside = F()) {
   const DownColumns<T, D> columns(tile, row0, lane);
-  Ahead<T> ahead;
+  Ahead<T, kAhead<D>> ahead;
   ahead.start(columns);
   const Frag<T> f[2] = {from_acc<T>(w, 0), from_acc<T>(w, 1)};
-  ahead.template run<D / 16>(columns, [&](int n, const Frag<T>& u) { acc[n % (D / 32)] = mma(u, f[n / (D / 32)], acc[n % (D / 32)]); });
+  ahead.template run<D / 16>(columns, [&](int n, const Frag<T>& u) { acc[n % (D / 32)] = mma(u, f[n / (D / 32)], acc[n % (D / 32)]); }, beside);
 }
 // LDS accesses of a wavefront are carried out in order: nothing is to be moved across, that is all
 __device__ __forceinline__ void wave_fence() { asm volatile("" ::: "memory"); }
@@ -475,17 +487,17 @@ __global__ __launch_bounds__(kThreads, (kForwardWaves<T, D, RB>)) void seq_fwd_k
           for (int r = 0; r < 16; ++r) o[e][r] *= f;
       }
       const float mc = m == -INFINITY ? 0.f : m * c;
-      float sum = 0.f;
+      const auto exponential = [&](int t, int r) {
+        p[t][r] = __builtin_amdgcn_exp2f(fmaf(p[t][r], c, -mc));
+        l += p[t][r];
+      };
+#pragma unroll
+      for (int r = 0; r < 16; ++r) exponential(0, r);
 #pragma unroll
       for (int t = 0; t < NS; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          p[t][r] = __builtin_amdgcn_exp2f(fmaf(p[t][r], c, -mc));
-          sum += p[t][r];
-        }
-      l += sum;
-#pragma unroll
-      for (int t = 0; t < NS; ++t) add_rows<T, D>(o, Vs, base + 32 * t, lane, p[t]);
+        add_rows<T, D>(o, Vs, base + 32 * t, lane, p[t], [&](int n) {
+          if (t + 1 < NS) part_of_16<D>(n, [&](int r) { exponential(t + 1, r); });
+        });
     }
     __syncthreads();
   }
@@ -621,6 +633,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
     df[kk] = load8(static_cast<const T*>(a.dout) + o_at + 16 * kk);
     oo = mma(load8(static_cast<const T*>(a.out) + o_at + 16 * kk), df[kk], oo);  // [row of out][row of d_out]
   }
+  const float c = a.scale * kLog2e;
   float delta = 0.f;  // the diagonal: row col, in the half that holds it
 #pragma unroll
   for (int r = 0; r < 16; ++r) delta = row_of(r, half) == col ? oo[r] : delta;
@@ -629,7 +642,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
     if (((col >> 2) & 1) != half) delta = other;
   }
   const float lse2 = a.lse[stat] * kLog2e;
-  if (row < rows && half == 0 && (RB > 32 || wave == 0)) reinterpret_cast<float2*>(a.delta)[((int64_t)head * a.q_rows + s.q0) * group + row] = make_float2(lse2, delta);
+  if (row < rows && half == 0 && (RB > 32 || wave == 0)) reinterpret_cast<float2*>(a.delta)[((int64_t)head * a.q_rows + s.q0) * group + row] = make_float2(lse2 == -INFINITY ? -INFINITY : -lse2 / c, delta);
   const int lo = key_begin(a, s, token), hi = row < rows ? key_end(a, s, token) : 0;
   const int t_first = a.group.of(r0), t_last = a.group.of(min(r0 + RB, rows) - 1);
   const int j_lo = key_begin(a, s, t_first), j_hi = key_end(a, s, t_last);
@@ -641,7 +654,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
   f32x16_t dq[D / 32];
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) dq[e] = zero16();
-  const float c = a.scale * kLog2e;
   Stage<T, D, KT> ks, vs;
   const auto load = [&](int j) {
     ks.load(kp, a.ld_k, j, s.kn);
@@ -658,10 +670,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
       const int at = RB == 32 ? 32 * wave : 32 * t, j = j0 + at;
       if (j >= any_hi || j + 32 <= any_lo) continue;
       f32x16_t p = rows_times<T, D>(Ks, at, lane, [&](int kk) { return qf[kk]; });
-      f32x16_t dp = rows_times<T, D>(Vs, at, lane, [&](int kk) { return df[kk]; });
+      const bool whole = j >= w_lo && j + 32 <= w_hi;
+      f32x16_t dp = rows_times<T, D>(Vs, at, lane, [&](int kk) { return df[kk]; },
+                                     [&](int n) { part_of_16<D>(n, [&](int r) { p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, -lse2)); }); });
 #pragma unroll
-      for (int r = 0; r < 16; ++r) dp[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, -lse2)) * (dp[r] - delta);
-      if (j < w_lo || j + 32 > w_hi) {
+      for (int r = 0; r < 16; ++r) dp[r] = p[r] * (dp[r] - delta);
+      if (!whole) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = j + row_of(r, half);
@@ -705,7 +719,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
 //   <128, 1>  many blocks, in which starts and ends of some hide behind others.
 //   <32, 4>   fewer blocks than compute units.
 // Tiles are written to LDS one step ahead, so that there is one barrier a step.
-// fragments of the values (of D / 16) that lie in LDS, a thread's own, since the registers do not hold them
+// fragments of the keys and of the values (of D / 16) that lie in LDS, a thread's own, since the registers do not hold them; read ahead like
+// the tiles (the compiler's own choice, memory, is read when it is wanted: 590 -> 715 us for two fragments)
+template <class T, int D>
+constexpr int kKeysInLds = sizeof(T) == 2 && D == 128 ? 2 : 0;
 template <class T, int D>
 constexpr int kValuesInLds = sizeof(T) == 2 ? D == 128 ? 8 : D == 64 ? 4 : 0 : 0;
 // rows of a wavefront's tile
@@ -713,7 +730,7 @@ template <class T, int D>
 constexpr int kQueryTile = sizeof(T) == 2 && D == 32 ? 64 : 32;
 
 template <class T, int D, int RB, int P>
-__global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64) ? 1 : D == 128 || P > 1 ? 2 : 3) void seq_bwd_k_k(SeqAttn a) {
+__global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64) ? 1 : D == 128 || RB == 32 ? 2 : 3) void seq_bwd_k_k(SeqAttn a) {
   constexpr int NT = 2 * RB * P, WT = kQueryTile<T, D>, QT = WT * P, S = kStride<T, D>;
   constexpr int kTileBytes = 4 * QT * S * (int)sizeof(T), kMergeBytes = (P - 1) * RB * D * 4;
   __shared__ __attribute__((aligned(256))) char tiles[kTileBytes > kMergeBytes ? kTileBytes : kMergeBytes];
@@ -721,7 +738,7 @@ __global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64)
   const auto Cs = [&](int buf) { return reinterpret_cast<T*>(tiles) + (2 + buf) * QT * S; };
   constexpr int VL = RB == 32 ? 0 : kValuesInLds<T, D>, VR = D / 16 - VL;
   __shared__ Frag<T> v_lds[VL > 0 ? VL : 1][VL > 0 ? NT : 1];
-  __shared__ __attribute__((aligned(16))) float stats[2][2][QT];  // log-sum-exp times log2(e), delta
+  __shared__ __attribute__((aligned(16))) float stats[2][2][QT];  // -lse / scale, delta
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = w % (RB / 32), part = w / (RB / 32);
   const int group = a.group.d, head = blockIdx.x % a.hk;
@@ -733,10 +750,13 @@ __global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64)
   const int key = j0 + 32 * wave + col, kc = min(key, s.kn - 1);
   const T* kp = static_cast<const T*>(a.k) + (s.k0 + kc) * a.ld_k + head * D + 8 * half;
   const T* vp = static_cast<const T*>(a.v) + (s.k0 + kc) * a.ld_v + head * D + 8 * half;
-  Frag<T> kf[D / 16], vf[VR > 0 ? VR : 1];
+  constexpr int KL = RB == 32 ? 0 : kKeysInLds<T, D>, KR = D / 16 - KL;
+  __shared__ Frag<T> k_lds[KL > 0 ? KL : 1][KL > 0 ? NT : 1];
+  Frag<T> kf[KR], vf[VR > 0 ? VR : 1];
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) {
-    kf[kk] = load8(kp + 16 * kk);
+    if (kk < KR) kf[kk] = load8(kp + 16 * kk);
+    else k_lds[kk - KR][threadIdx.x] = load8(kp + 16 * kk);
     if (kk < VR) vf[kk] = load8(vp + 16 * kk);
     else v_lds[kk - VR][threadIdx.x] = load8(vp + 16 * kk);
   }
@@ -790,19 +810,51 @@ __global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64)
     for (int t = 0; t < WT / 32; ++t) {
       const int at_t = part * WT + 32 * t, rt = r + at_t;
       if (rt >= any_hi || rt + 32 <= any_lo) continue;
-      f32x16_t p = rows_times<T, D>(Qs(buf), at_t, lane, [&](int kk) { return kf[kk]; });
-      f32x16_t dp = rows_times<T, D>(Cs(buf), at_t, lane, [&](int kk) { return kk < VR ? vf[kk < VR ? kk : 0] : v_lds[kk < VR ? 0 : kk - VR][VL > 0 ? threadIdx.x : 0]; });
+      const float* st = &stats[buf][0][at_t + 4 * half];
+      f32x16_t p;  // starts at -lse / scale: nothing is left to subtract
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 ls = *reinterpret_cast<const float4*>(&stats[buf][0][at_t + 8 * i + 4 * half]);
-        const float4 de = *reinterpret_cast<const float4*>(&stats[buf][1][at_t + 8 * i + 4 * half]);
-        const float lsv[4] = {ls.x, ls.y, ls.z, ls.w}, dev[4] = {de.x, de.y, de.z, de.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          p[4 * i + j] = __builtin_amdgcn_exp2f(fmaf(p[4 * i + j], c, -lsv[j]));
-          dp[4 * i + j] = p[4 * i + j] * (dp[4 * i + j] - dev[j]);
-        }
+      for (int i = 0; i < 16; i += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(st + 2 * i);
+        p[i] = v.x;
+        p[i + 1] = v.y;
+        p[i + 2] = v.z;
+        p[i + 3] = v.w;
       }
+      Frag<T> kl[KL > 0 ? KL : 1];
+      p = rows_times<T, D>(
+          Qs(buf), at_t, lane, [&](int kk) { return kk < KR ? kf[kk < KR ? kk : 0] : kl[kk < KR ? 0 : kk - KR]; },
+          [&](int n) {
+            if (n < KL) kl[n] = k_lds[n][threadIdx.x];
+          },
+          p);
+      const auto exponentials = [&](int n) { part_of_16<D>(n, [&](int i) { p[i] = __builtin_amdgcn_exp2f(p[i] * c); }); };
+      f32x16_t dp = zero16();
+      if constexpr (VL == 0) {
+        dp = rows_times<T, D>(Cs(buf), at_t, lane, [&](int kk) { return vf[kk]; }, exponentials);
+      } else {  // both operands come from LDS: two of either ahead
+        static_assert(VL == D / 16, "all of them");
+        const AlongRows<T, D> of_c(Cs(buf), at_t, lane);
+        const auto of_v = [&](int kk) { return v_lds[kk][threadIdx.x]; };
+        Ahead<T, 2> c_ahead;
+        Frag<T> v_ahead[2] = {of_v(0), of_v(1)};
+        c_ahead.start(of_c);
+        c_ahead.template run<D / 16>(
+            of_c,
+            [&](int kk, const Frag<T>& f) {
+              dp = mma(f, v_ahead[kk % 2], dp);
+              if (kk + 2 < D / 16) v_ahead[kk % 2] = of_v(kk + 2);
+            },
+            exponentials);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(st + QT + 2 * i);
+        dp[i] = p[i] * (dp[i] - v.x);
+        dp[i + 1] = p[i + 1] * (dp[i + 1] - v.y);
+        dp[i + 2] = p[i + 2] * (dp[i + 2] - v.z);
+        dp[i + 3] = p[i + 3] * (dp[i + 3] - v.w);
+      }
+      __builtin_amdgcn_sched_barrier(0);
       if (rt < w_lo || rt + 32 > w_hi) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -891,9 +943,10 @@ void backward(const SeqAttn& a, hipStream_t st) {
   if (kSmall && n < kUnits) {
     if constexpr (kSmall) seq_bwd_k_k<T, D, 32, 4><<<(unsigned)(slots(a.k_rows, a.batch, 1, 32) * a.hk), 256, 0, st>>>(a);
   } else if (sizeof(T) == 2 && (D == 128 || n < 3 * kUnits)) {
-    if constexpr (sizeof(T) == 2) seq_bwd_k_k<T, D, 128, 2><<<(unsigned)n, 512, 0, st>>>(a);
+    constexpr int P = D == 128 ? 2 : 3;
+    if constexpr (sizeof(T) == 2) seq_bwd_k_k<T, D, 128, P><<<(unsigned)n, 256 * P, 0, st>>>(a);
   } else {
-    seq_bwd_k_k<T, D, 128, 1><<<(unsigned)n, 256, 0, st>>>(a);
+    if constexpr (sizeof(T) == 4 || D < 128) seq_bwd_k_k<T, D, 128, 1><<<(unsigned)n, 256, 0, st>>>(a);
   }
 }
 
