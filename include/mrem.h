@@ -342,7 +342,7 @@ mrem_status mrem_rotary_backward(const void* dy, void* dx, int32_t dtype, int64_
  *                       checked: they are cut to the rows that there are, a length also to the next start
  *   lse                 device fp32 [q_heads, q_rows]
  * Rows of no sequence are neither read nor written (out, lse and the gradients keep what they held there).  A value that is not
- * finite reaches only queries and keys that see it or lie in the same tile of up to 128.
+ * finite reaches what sees it and nothing else.
  * head_dim 32, 64 or 128; q_heads a multiple of kv_heads; q_rows * (q_heads / kv_heads) and k_rows < 2^31 - 2^20, and each of
  * them / 32, plus batch, times kv_heads < 2^24; strides
  * multiples of 16 bytes, at least heads * head_dim and at most 2^21; pointers 16-byte aligned.  Outputs may not overlap inputs.

@@ -393,6 +393,103 @@ __device__ __forceinline__ void store_rows(T* scratch, const f32x16_t (&acc)[D /
   }
 }
 
+// ---- values that are not finite ----------------------------------------------
+// A matrix instruction multiplies what a query does not see by zero, and zero times an infinity is not a number.  So a result that is not finite
+// is formed again, from what is seen only, wherever it need not be so: by a wavefront a row, value by value.  Such rows are rare (a sum
+// that is not a number in all its values is given up on the way), and finite results pay for a test.
+template <int D>
+__device__ __forceinline__ bool not_finite(const f32x16_t (&acc)[D / 32]) {
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) bad |= !(fabsf(acc[e][r]) < INFINITY);
+  return bad;
+}
+// rows of a tile, a bit each, for which either half's lane says so
+__device__ __forceinline__ unsigned rows_where(bool lane_says) {
+  const unsigned long long m = __ballot(lane_says);
+  return (unsigned)m | (unsigned)(m >> 32);
+}
+// a row of D values in the lanes of a wavefront
+template <class T, int D>
+struct LaneRow {
+  static constexpr int kN = (D + 63) / 64;
+  float v[kN];
+  __device__ __forceinline__ explicit LaneRow(const T* p) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int d = (threadIdx.x & 63) + 64 * i;
+      v[i] = d < D ? (float)p[d] : 0.f;
+    }
+  }
+  __device__ __forceinline__ float dot(const LaneRow& o) const {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) t += v[i] * o.v[i];
+    return wave_sum(t);
+  }
+};
+template <int N>
+struct LaneSum {
+  float v[N] = {};
+  template <class R>
+  __device__ __forceinline__ void add(float f, const R& r) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += f * r.v[i];
+  }
+  __device__ __forceinline__ bool lost() const {  // not a number in any lane
+    bool all = true;
+#pragma unroll
+    for (int i = 0; i < N; ++i) all &= v[i] != v[i];
+    return __all(all);
+  }
+  template <class T>
+  __device__ __forceinline__ void store(T* p, float f, int n) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int d = (threadIdx.x & 63) + 64 * i;
+      if (d < n) p[d] = static_cast<T>(v[i] * f);
+    }
+  }
+};
+// the output of a (token, head) from its log-sum-exp, and with GRADIENT that of its query
+template <class T, int D, bool GRADIENT>
+__device__ __forceinline__ void query_again(const SeqAttn& a, const Seq& s, int head, int h, int token, float lse, float delta) {
+  const T *kp = static_cast<const T*>(a.k) + s.k0 * a.ld_k + head * D, *vp = static_cast<const T*>(a.v) + s.k0 * a.ld_v + head * D;
+  const LaneRow<T, D> q(static_cast<const T*>(a.q) + (s.q0 + token) * a.ld_q + h * D);
+  const LaneRow<T, D> c(static_cast<const T*>(GRADIENT ? a.dout : a.q) + (s.q0 + token) * (GRADIENT ? a.ld_o : a.ld_q) + h * D);
+  LaneSum<LaneRow<T, D>::kN> sum;
+  const int end = key_end(a, s, token);
+#pragma unroll 1
+  for (int j = key_begin(a, s, token); j < end && !sum.lost(); ++j) {
+    const LaneRow<T, D> k(kp + j * a.ld_k), v(vp + j * a.ld_v);
+    const float p = __builtin_amdgcn_exp2f((q.dot(k) * a.scale - lse) * kLog2e);
+    if constexpr (GRADIENT) sum.add(p * (c.dot(v) - delta), k);
+    else sum.add(p, v);
+  }
+  if constexpr (GRADIENT) sum.store(static_cast<T*>(a.dq) + (s.q0 + token) * a.ld_q + h * D, a.scale, D);
+  else sum.store(static_cast<T*>(a.out) + (s.q0 + token) * a.ld_o + h * D, 1.f, D);
+}
+// the gradients of a key and its value: rows [lo, hi) of the packed axis see it
+template <class T, int D>
+__device__ __forceinline__ void key_again(const SeqAttn& a, const Seq& s, int head, int key, int lo, int hi) {
+  const LaneRow<T, D> k(static_cast<const T*>(a.k) + (s.k0 + key) * a.ld_k + head * D), v(static_cast<const T*>(a.v) + (s.k0 + key) * a.ld_v + head * D);
+  const float2* stats = reinterpret_cast<const float2*>(a.delta) + ((int64_t)head * a.q_rows + s.q0) * a.group.d;
+  LaneSum<LaneRow<T, D>::kN> dk, dv;
+#pragma unroll 1
+  for (int r = lo; r < hi && !(dk.lost() && dv.lost()); ++r) {
+    const int t = a.group.of(r), h = head * a.group.d + r - t * a.group.d;
+    const LaneRow<T, D> q(static_cast<const T*>(a.q) + (s.q0 + t) * a.ld_q + h * D), c(static_cast<const T*>(a.dout) + (s.q0 + t) * a.ld_o + h * D);
+    const float2 st = stats[r];
+    const float p = __builtin_amdgcn_exp2f((q.dot(k) + st.x) * a.scale * kLog2e);
+    dv.add(p, c);
+    dk.add(p * (c.dot(v) - st.y), q);
+  }
+  dk.store(static_cast<T*>(a.dk) + (s.k0 + key) * a.ld_k + head * D, a.scale, D);
+  dv.store(static_cast<T*>(a.dv) + (s.k0 + key) * a.ld_v + head * D, 1.f, D);
+}
+
 // ---- forward -----------------------------------------------------------------
 // rows of a block: 128, 32 a wavefront, keys in tiles of 64 (fp32: 32); or 32 that all wavefronts share, each with 32 of a tile's
 // 128 keys, for sequences with few queries: what a block then does is read keys, and it reads four times as many at a time
@@ -564,9 +661,17 @@ __global__ __launch_bounds__(kThreads, (kForwardWaves<T, D, RB>)) void seq_fwd_k
       return place(r, &rh, &rt) ? a.part + (((int64_t)split * a.hq + rh) * a.q_rows + s.q0 + rt) * D : nullptr;
     });
   } else {
+    const unsigned again = rows_where(row < rows && l > 0.f && l < INFINITY && not_finite<D>(o));
     store_rows<T, D>(reinterpret_cast<T*>(lds) + (RB == 32 ? 0 : wave * 32 * S), o, l == 0.f ? 0.f : 1.f / l, lane, [&](int r) {
-      return place(r, &rh, &rt) ? static_cast<T*>(a.out) + (s.q0 + rt) * a.ld_o + rh * D : nullptr;
+      return place(r, &rh, &rt) && !(again >> r & 1) ? static_cast<T*>(a.out) + (s.q0 + rt) * a.ld_o + rh * D : nullptr;
     });
+    const float lse = (m * c + log2f(l)) * kLn2;
+#pragma unroll 1
+    for (unsigned left = again; left; left &= left - 1) {
+      const int r = __builtin_ctz(left);
+      place(r, &rh, &rt);
+      query_again<T, D, false>(a, s, head, rh, rt, __shfl(lse, r), 0.f);
+    }
   }
 }
 
@@ -598,11 +703,19 @@ __global__ __launch_bounds__(kThreads) void seq_join_k(SeqAttn a) {
           if (lane + 64 * e < D) o[e] += part[lane + 64 * e] * w;
       }
     const float f = l == 0.f ? 0.f : 1.f / l;
+    const float lse = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
+    if (lane == 0) a.lse[at] = lse;
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < (D + 63) / 64; ++e) bad |= !(fabsf(o[e]) < INFINITY);
+    if (__any(bad) && fabsf(lse) < INFINITY) {
+      query_again<T, D, false>(a, s, head, h, token, lse, 0.f);
+      continue;
+    }
     T* out = static_cast<T*>(a.out) + (s.q0 + token) * a.ld_o + h * D;
 #pragma unroll
     for (int e = 0; e < (D + 63) / 64; ++e)
       if (lane + 64 * e < D) out[lane + 64 * e] = static_cast<T>(o[e] * f);
-    if (lane == 0) a.lse[at] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * kLn2;
   }
 }
 
@@ -704,10 +817,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
         for (int r = 0; r < 16; ++r) dq[e][r] += x[(w - 1) * 32 * D + (e * 16 + r) * 64];
   }
   if constexpr (RB == 32) wave_fence();  // the sums have been read
+  const unsigned again = rows_where(row < rows && fabsf(lse2) < INFINITY && fabsf(delta) < INFINITY && not_finite<D>(dq));
   store_rows<T, D>(tiles + (RB == 32 ? 0 : wave * 32 * S), dq, a.scale, lane, [&](int r) -> T* {
     const int at = wr + r, t = a.group.of(at);
-    return at < rows ? static_cast<T*>(a.dq) + (s.q0 + t) * a.ld_q + (head * group + at - t * group) * D : nullptr;
+    return at < rows && !(again >> r & 1) ? static_cast<T*>(a.dq) + (s.q0 + t) * a.ld_q + (head * group + at - t * group) * D : nullptr;
   });
+#pragma unroll 1
+  for (unsigned left = again; left; left &= left - 1) {
+    const int r = __builtin_ctz(left), at = wr + r, t = a.group.of(at);
+    query_again<T, D, true>(a, s, head, head * group + at - t * group, t, __shfl(lse2, r) * kLn2, __shfl(delta, r));
+  }
 }
 
 // Gradients of keys and values: RB keys a block, 32 a wavefront, the queries of all heads of the group in tiles of rows.  P wavefronts own
@@ -897,11 +1016,17 @@ __global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64)
   if constexpr (P > 1) wave_fence();  // the sums have been read; their place is this wavefront's own
   T* scratch = reinterpret_cast<T*>(tiles) + wave * (P > 1 ? 32 * D * 4 / (int)sizeof(T) : 32 * S);
   static_assert(P > 1 ? 32 * D * 4 >= 32 * S * (int)sizeof(T) || sizeof(T) == 4 : kTileBytes >= RB * S * (int)sizeof(T) || sizeof(T) == 4, "rows are put together where the tiles were");
+  const unsigned again = rows_where(key < s.kn && (not_finite<D>(dk) || not_finite<D>(dv)));
   const auto rows_of = [&](void* base, int64_t ld) {
-    return [=](int r) -> T* { return j0 + 32 * wave + r < s.kn ? static_cast<T*>(base) + (s.k0 + j0 + 32 * wave + r) * ld + head * D : nullptr; };
+    return [=](int r) -> T* { return j0 + 32 * wave + r < s.kn && !(again >> r & 1) ? static_cast<T*>(base) + (s.k0 + j0 + 32 * wave + r) * ld + head * D : nullptr; };
   };
   store_rows<T, D>(scratch, dk, a.scale, lane, rows_of(a.dk, a.ld_k));
   store_rows<T, D>(scratch, dv, 1.f, lane, rows_of(a.dv, a.ld_v));
+#pragma unroll 1
+  for (unsigned left = again; left; left &= left - 1) {
+    const int j = j0 + 32 * wave + __builtin_ctz(left);
+    key_again<T, D>(a, s, head, j, row_begin(j), row_end(j));
+  }
 }
 
 // ---- launches ----------------------------------------------------------------

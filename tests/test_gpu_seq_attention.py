@@ -224,6 +224,53 @@ def test_gradients_against_differences(env):
         assert abs((sides[0] - sides[1]) / (2 * e) - want) < 2e-3 * max(1.0, abs(want)), name
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("q_lens,k_lens,hq,hk,d,window", [([150], [150], 4, 2, 64, 0), ([150], [150], 2, 2, 128, 40), ([1, 3], [700, 300], 8, 2, 128, 90), ([9000], [9000], 8, 8, 32, 33)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_what_is_not_finite_reaches_what_sees_it_only(env, q_lens, k_lens, hq, hk, d, window, bad, dtype):
+    """one key, value, query and output gradient each: what does not see it gives what it gives without"""
+    torch, B = env
+    names = ("out", "lse", "dq", "dk", "dv")
+    t = case_tensors(torch, B, q_lens, k_lens, hq, hk, d, dtype, 1, window, "packed")
+    run(B, t)
+    want = {n: t[n].clone() for n in names}
+    off, q_at, k_at = k_lens[0] - q_lens[0], q_lens[0] // 2, (k_lens[0] - q_lens[0]) + q_lens[0] // 2
+    token, key = torch.arange(t["q"].shape[0], device="cuda"), torch.arange(t["k"].shape[0], device="cuda")
+    sees = (token < q_lens[0]) & (token + off >= k_at) & ((window == 0) | (token + off - (window or 0) < k_at))    # queries that see the key
+    seen = (key < k_lens[0]) & (key <= q_at + off) & ((window == 0) | (key > q_at + off - (window or 0)))          # keys that the query sees
+    # rows formed again do without one rounding of their operands: as far off as the module's tests allow, element by element
+    tol = 2e-2 if dtype == "bfloat16" else 1e-4
+    close = lambda a, b: ((a.float() - b.float()).abs() <= tol * (b.float().abs() + b.float().abs().max())).all()  # noqa: E731
+    for name, at in (("v", k_at), ("k", k_at), ("q", q_at), ("dout", q_at)):
+        kept = t[name][at, 0].clone()
+        t[name][at, 0, 3] = bad
+        run(B, t)
+        t[name][at, 0] = kept
+        heads = hq // hk if name in ("k", "v") else 1
+        hit = sees if name in ("k", "v") else token == q_at                                       # rows of these heads
+        # the queries' side: what the poisoned heads' other rows, and all other heads, give
+        for n in ("out", "dq"):
+            clean = torch.ones(t[n].shape[:2], dtype=torch.bool, device="cuda")
+            clean[:, :heads] = ~hit[:, None]
+            assert torch.isfinite(t[n].float()[clean]).all() and close(t[n][clean], want[n][clean]), (name, n)
+        # the keys' side: those that no hit query sees
+        reached = seen if name in ("q", "dout") else torch.zeros_like(key, dtype=torch.bool)
+        if name in ("k", "v"):
+            first, last = int(token[sees].min()) if sees.any() else 0, int(token[sees].max()) if sees.any() else -1
+            reached = (key < k_lens[0]) & (key <= last + off) & ((window == 0) | (key > first + off - (window or 0))) & bool(sees.any())
+        for n in ("dk", "dv"):
+            clean = torch.ones(t[n].shape[:2], dtype=torch.bool, device="cuda")
+            clean[:, 0] = ~reached
+            assert torch.isfinite(t[n].float()[clean]).all() and close(t[n][clean], want[n][clean]), (name, n)
+        # and it does arrive
+        if name == "v":
+            assert not torch.isfinite(t["out"][hit][:, :heads, 3].float()).any()
+        if name == "dout":
+            assert not torch.isfinite(t["dv"][seen][:, 0, 3].float()).any()
+    run(B, t)
+    assert all(torch.equal(t[n], want[n]) for n in names)
+
+
 def test_no_sequence_has_rows(env):
     torch, B = env
     t = case_tensors(torch, B, [0, 0], [0, 0], 2, 1, 64, "bfloat16", 1, 0, "packed")
