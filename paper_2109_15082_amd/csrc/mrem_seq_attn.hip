@@ -832,11 +832,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
 // Gradients of keys and values: RB keys a block, 32 a wavefront, the queries of all heads of the group in tiles of rows.  P wavefronts own
 // the same keys, take every P-th tile, and meet in LDS at the end.  Both gradients, both operands and two tiles of scores are some 230
 // registers a lane at head dimension 128, which allows two wavefronts a SIMD.
-//   <128, 2>  few blocks a compute unit: the two wavefronts of a SIMD share their keys.  With other keys for the second one there would be
-//             half as many blocks, each twice as long, and under a causal mask the block of the first keys would outlast the others by half
-//             of the kernel's time (2 x 4096 tokens, 32 heads on 8, 128 wide: 690 against 1230 us).
-//   <128, 1>  many blocks, in which starts and ends of some hide behind others.
-//   <32, 4>   fewer blocks than compute units.
+//   <32, 4>   fewer blocks of 128 keys than compute units.  us of a backward pass, against <128, 2>: 34 blocks (2048 tokens, 8 heads on 2, 128
+//             wide) 185 against 291, 132 (2 x 4096) 455 against 618, 108 (1024 tokens, 12 heads of 64) 41 against 48; 272 (128 wide) 406
+//             against 354, 324 (64 wide) 58 against 51.
+//   <128, 2>  (128 wide), <128, 3> (narrower, up to two blocks a unit): the wavefronts of a SIMD share their keys.  With other keys for the second
+//             one there would be half as many blocks, each twice as long, and under a causal mask the block of the first keys
+//             would outlast the others by half of the kernel's time (2 x 4096 tokens, 32 heads on 8, 128 wide: 690 against 1230 us).
+//   <128, 1>  (narrower, more blocks): starts and ends of some hide behind others; 432 blocks of 12 heads of 64: 64 against 66 us with
+//             <128, 3>, 864: 84 against 98, 3456: 262 against 329.
 // Tiles are written to LDS one step ahead, so that there is one barrier a step.
 // fragments of the keys and of the values (of D / 16) that lie in LDS, a thread's own, since the registers do not hold them; read ahead like
 // the tiles (the compiler's own choice, memory, is read when it is wanted: 590 -> 715 us for two fragments)
@@ -1032,16 +1035,20 @@ __global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64)
 // ---- launches ----------------------------------------------------------------
 constexpr int kUnits = 256;  // compute units
 // Blocks of 128 rows while there is one for each compute unit.  Below that, and where a sequence has on the average fewer rows than
-// half a block (the lengths are not known on the host), blocks of 32 rows, whose wavefronts share out the keys.
+// half a block (the lengths are not known on the host), blocks of 32 rows, whose wavefronts share out the keys.  us, 128 rows against 32:
+// 130 blocks of 128 (2048 tokens, 8 heads on 2, 128 wide) 49 against 33 forward, 216 (2 x 1024 tokens, 12 heads of 64) 20 against 16; 324 of
+// those 21 and 21, query gradients equal too; 516 (2 x 4096, 8 heads on 2, 128 wide) 137 against 150.
 bool few_rows(const SeqAttn& a) {
   const int64_t group = a.hq / a.hk;
   return slots(a.q_rows, a.batch, (int)group, 128) * a.hk < kUnits || a.q_rows * group <= (int64_t)64 * a.batch;
 }
-// keys are shared out among blocks while there are fewer than four blocks a compute unit, each keeping two tiles
+// With fewer blocks of 32 rows than compute units keys are shared out among blocks too, up to four blocks a unit, each keeping two tiles: the
+// case of single tokens (16 of them on up to 8192 keys, 8 key heads of 128: 7 parts; one would leave 112 units idle).  With a block
+// for each unit a second launch that joins the parts costs more than it gives (1024 tokens, 8 heads on 2: 30 us with three parts, 27 with none).
 int splits(const SeqAttn& a) {
   if (!few_rows(a) || a.q_rows == 0) return 1;
   const int64_t blocks = slots(a.q_rows, a.batch, a.hq / a.hk, 32) * a.hk, keys = (a.k_rows + a.batch - 1) / a.batch;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({4 * kUnits / blocks, keys / 256, 32}));
+  return blocks >= kUnits ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({4 * kUnits / blocks, keys / 256, 32}));
 }
 
 template <class T, int D>
@@ -1067,7 +1074,7 @@ void backward(const SeqAttn& a, hipStream_t st) {
   constexpr bool kSmall = sizeof(T) == 2 || D < 128;  // what LDS and registers hold
   if (kSmall && n < kUnits) {
     if constexpr (kSmall) seq_bwd_k_k<T, D, 32, 4><<<(unsigned)(slots(a.k_rows, a.batch, 1, 32) * a.hk), 256, 0, st>>>(a);
-  } else if (sizeof(T) == 2 && (D == 128 || n < 3 * kUnits)) {
+  } else if (sizeof(T) == 2 && (D == 128 || n < 2 * kUnits)) {
     constexpr int P = D == 128 ? 2 : 3;
     if constexpr (sizeof(T) == 2) seq_bwd_k_k<T, D, 128, P><<<(unsigned)n, 256 * P, 0, st>>>(a);
   } else {

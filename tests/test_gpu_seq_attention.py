@@ -15,7 +15,10 @@ def env():
     import torch
     assert torch.cuda.is_available(), "these tests need the GPU"
     from paper_2109_15082_amd import binding as B
-    return torch, B
+    default = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)  # what other modules of a run have set is no matter here
+    yield torch, B
+    torch.set_default_dtype(default)
 
 
 def case_tensors(torch, B, q_lens, k_lens, hq, hk, d, dtype, causal, window, layout, seed=0, scale=None, spare=3):
