@@ -378,12 +378,16 @@ _DTYPES = {torch.bfloat16: MREM_BF16, torch.float32: MREM_FP32}
 _TYPES = {v: k for k, v in _DTYPES.items()}
 
 
-def _heads(t: torch.Tensor, name: str) -> None:
-    """t is a [rows, heads, head_dim] view whose heads are contiguous; rows may lie any distance apart."""
-    if t.dim() != 3 or t.dtype not in _DTYPES:
+def _heads(t: torch.Tensor, name: str) -> int:
+    """Elements between the rows of a [rows, heads, head_dim] view whose heads are contiguous; rows may lie any distance apart."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or t.dtype not in _DTYPES:
         raise ValueError(f"{name}: bf16 or fp32 [rows, heads, head_dim] expected")
-    if t.numel() and not ((t.stride(2) == 1 or t.shape[2] == 1) and (t.stride(1) == t.shape[2] or t.shape[1] == 1)):
-        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    rows, heads, dim = shape
+    if stride[2] != 1 or stride[1] != dim:  # unless those that differ are of a single value or head, or of nothing
+        if rows * heads * dim and not ((stride[2] == 1 or dim == 1) and (stride[1] == dim or heads == 1)):
+            raise ValueError(f"{name}: the heads of a row must be contiguous")
+    return stride[0] if rows > 1 else heads * dim  # of a single row or none, its width
 
 
 def _row_stride(t: torch.Tensor) -> int:
@@ -402,6 +406,9 @@ def _plain(t: Optional[torch.Tensor], name: str, dtype, shape):
     return t.data_ptr() or None
 
 
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _run(fn, stream, tensors, *args) -> None:
     """fn(*args, stream) on the tensors' device, where it is not the current one too."""
     device = tensors[0].get_device()
@@ -410,10 +417,12 @@ def _run(fn, stream, tensors, *args) -> None:
             raise ValueError(f"the tensors are on several devices: {sorted({str(t.device) for t in tensors if t is not None})}")
     if device < 0:
         raise ValueError("device tensors required")
-    if device != torch.cuda.current_device():
+    if device != _current_device():
         with torch.cuda.device(device):
             return _check(fn(*args, _stream(stream)))
-    _check(fn(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)))
+    status = fn(*args, _raw_stream(device) if stream is None else _stream(stream))
+    if status != MREM_OK:
+        _check(status)
 
 
 def mrem_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int = MREM_ROTARY_PLAIN, factor: float = 1.0,
@@ -425,14 +434,12 @@ def mrem_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int
 
 
 def _rotary(fn, x, y, rotary_dim, interleaved, amplitude, freq, positions, seq, stream):
-    _heads(x, "x")
-    _heads(y, "y")
-    shape = x.shape
+    ld_x, ld_y, shape = _heads(x, "x"), _heads(y, "y"), x.shape
     if y.shape != shape or y.dtype is not x.dtype:
         raise ValueError("x and y must have one shape and type")
     rows, heads, dim = shape
-    _run(fn, stream, (x, y, freq, positions), x.data_ptr() or None, y.data_ptr() or None, _DTYPES[x.dtype], rows, heads, dim, _row_stride(x),
-         _row_stride(y), rotary_dim, int(interleaved), amplitude, _plain(freq, "freq", torch.float64, (rotary_dim // 2,)),
+    _run(fn, stream, (x, y, freq, positions), x.data_ptr() or None, y.data_ptr() or None, _DTYPES[x.dtype], rows, heads, dim, ld_x,
+         ld_y, rotary_dim, int(interleaved), amplitude, _plain(freq, "freq", torch.float64, (rotary_dim // 2,)),
          _plain(positions, "positions", torch.int32, (rows,)), (rows or 1) if seq is None else seq)
 
 

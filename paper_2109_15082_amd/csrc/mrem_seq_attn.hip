@@ -16,6 +16,7 @@
 #include "mrem_kernels.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace mrem {
 
@@ -932,6 +933,12 @@ __global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64)
     for (int t = 0; t < WT / 32; ++t) {
       const int at_t = part * WT + 32 * t, rt = r + at_t;
       if (rt >= any_hi || rt + 32 <= any_lo) continue;
+      // the wavefronts of a SIMD would fall into step, both at the matrix instructions and then both at the others: who is at them goes first
+      const auto priority = [](auto on) {
+        if constexpr (sizeof(T) == 2 && D == 128) __builtin_amdgcn_s_setprio(decltype(on)::value);
+      };
+      using First = std::integral_constant<short, 1>;
+      using Last = std::integral_constant<short, 0>;
       const float* st = &stats[buf][0][at_t + 4 * half];
       f32x16_t p;  // starts at -lse / scale: nothing is left to subtract
 #pragma unroll
@@ -943,6 +950,7 @@ __global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64)
         p[i + 3] = v.w;
       }
       Frag<T> kl[KL > 0 ? KL : 1];
+      priority(First());
       p = rows_times<T, D>(
           Qs(buf), at_t, lane, [&](int kk) { return kk < KR ? kf[kk < KR ? kk : 0] : kl[kk < KR ? 0 : kk - KR]; },
           [&](int n) {
@@ -968,6 +976,7 @@ __global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64)
             },
             exponentials);
       }
+      priority(Last());
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         const float4 v = *reinterpret_cast<const float4*>(st + QT + 2 * i);
@@ -987,8 +996,10 @@ __global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64)
           }
         }
       }
+      priority(First());
       add_rows<T, D>(dv, Cs(buf), at_t, lane, p);
       add_rows<T, D>(dk, Qs(buf), at_t, lane, dp);
+      priority(Last());
     }
     __syncthreads();
   }
