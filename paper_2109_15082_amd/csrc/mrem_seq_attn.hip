@@ -729,6 +729,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
   static_assert(2 * KT * S * (int)sizeof(T) >= (RB == 32 ? 32 * D * 4 * (kWaves - 1) : 0), "the sums meet where the tiles were");
   __shared__ __attribute__((aligned(256))) T tiles[2 * KT * S];
   T *const Ks = tiles, *const Vs = tiles + KT * S;
+  __shared__ float offs[kWaves][32];
   const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = a.group.d, head = blockIdx.x % a.hk;
   const int slot = (int)(gridDim.x / a.hk - 1 - blockIdx.x / a.hk);
@@ -756,7 +757,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
     if (((col >> 2) & 1) != half) delta = other;
   }
   const float lse2 = a.lse[stat] * kLog2e;
-  if (row < rows && half == 0 && (RB > 32 || wave == 0)) reinterpret_cast<float2*>(a.delta)[((int64_t)head * a.q_rows + s.q0) * group + row] = make_float2(lse2 == -INFINITY ? -INFINITY : -lse2 / c, delta);
   const int lo = key_begin(a, s, token), hi = row < rows ? key_end(a, s, token) : 0;
   const int t_first = a.group.of(r0), t_last = a.group.of(min(r0 + RB, rows) - 1);
   const int j_lo = key_begin(a, s, t_first), j_hi = key_end(a, s, t_last);
@@ -765,41 +765,66 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
 
   const T* kp = static_cast<const T*>(a.k) + s.k0 * a.ld_k + head * D;
   const T* vp = static_cast<const T*>(a.v) + s.k0 * a.ld_v + head * D;
-  f32x16_t dq[D / 32];
-#pragma unroll
-  for (int e = 0; e < D / 32; ++e) dq[e] = zero16();
   Stage<T, D, KT> ks, vs;
   const auto load = [&](int j) {
     ks.load(kp, a.ld_k, j, s.kn);
     vs.load(vp, a.ld_v, j, s.kn);
   };
-  if (j_lo < j_hi) load(j_lo);
-  for (int j0 = j_lo; j0 < j_hi; j0 += KT) {
-    ks.store(Ks);
-    vs.store(Vs);
-    __syncthreads();
-    if (j0 + KT < j_hi) load(j0 + KT);
+  // delta of a stored output is off by the output's rounding, which is what most of a row's gradient is made of where it sees few keys (a
+  // row's gradient is a difference of its few products).  There a first pass takes the sum of the score gradients, which is zero but for
+  // that error, back from delta: rows of up to 128 keys.  With more the error is below the rounding of the gradient itself.  (Two tokens
+  // of 128 wide heads in bf16: gradients 5.6e-3 off without it, 1.7e-3 with it; a row that sees one key has none, to the bit, in either type.)
+  const bool twice = (a.window ? min(a.window, j_hi) : j_hi) <= 128;
+  // gradients of the scores of keys [j, j + 32), rows `at` of the tile
+  const auto score_gradients = [&](int at, int j) {
+    f32x16_t p = rows_times<T, D>(Ks, at, lane, [&](int kk) { return qf[kk]; });
+    f32x16_t dp = rows_times<T, D>(Vs, at, lane, [&](int kk) { return df[kk]; },
+                                   [&](int n) { part_of_16<D>(n, [&](int r) { p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, -lse2)); }); });
 #pragma unroll
-    for (int t = 0; t < NS; ++t) {
-      const int at = RB == 32 ? 32 * wave : 32 * t, j = j0 + at;
-      if (j >= any_hi || j + 32 <= any_lo) continue;
-      f32x16_t p = rows_times<T, D>(Ks, at, lane, [&](int kk) { return qf[kk]; });
-      const bool whole = j >= w_lo && j + 32 <= w_hi;
-      f32x16_t dp = rows_times<T, D>(Vs, at, lane, [&](int kk) { return df[kk]; },
-                                     [&](int n) { part_of_16<D>(n, [&](int r) { p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, -lse2)); }); });
+    for (int r = 0; r < 16; ++r) dp[r] = p[r] * (dp[r] - delta);
+    if (j < w_lo || j + 32 > w_hi) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) dp[r] = p[r] * (dp[r] - delta);
-      if (!whole) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = j + row_of(r, half);
-          if (key < lo || key >= hi) dp[r] = 0.f;
-        }
+      for (int r = 0; r < 16; ++r) {
+        const int key = j + row_of(r, half);
+        if (key < lo || key >= hi) dp[r] = 0.f;
       }
-      add_rows<T, D>(dq, Ks, at, lane, dp);
     }
-    __syncthreads();
+    return dp;
+  };
+  const auto walk = [&](auto take) {
+    if (j_lo < j_hi) load(j_lo);
+    for (int j0 = j_lo; j0 < j_hi; j0 += KT) {
+      ks.store(Ks);
+      vs.store(Vs);
+      __syncthreads();
+      if (j0 + KT < j_hi) load(j0 + KT);
+#pragma unroll
+      for (int t = 0; t < NS; ++t) {
+        const int at = RB == 32 ? 32 * wave : 32 * t, j = j0 + at;
+        if (j < any_hi && j + 32 > any_lo) take(at, score_gradients(at, j));
+      }
+      __syncthreads();
+    }
+  };
+  if (twice) {
+    float off = 0.f;
+    walk([&](int, const f32x16_t& ds) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) off += ds[r];
+    });
+    off += other_half(off);
+    if constexpr (RB == 32) {  // each wavefront has seen a part of the keys
+      offs[wave][col] = off;
+      __syncthreads();
+      off = offs[0][col] + offs[1][col] + offs[2][col] + offs[3][col];
+    }
+    delta += off;
   }
+  f32x16_t dq[D / 32];
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) dq[e] = zero16();
+  walk([&](int at, const f32x16_t& ds) { add_rows<T, D>(dq, Ks, at, lane, ds); });
+  if (row < rows && half == 0 && (RB > 32 || wave == 0)) reinterpret_cast<float2*>(a.delta)[((int64_t)head * a.q_rows + s.q0) * group + row] = make_float2(lse2 == -INFINITY ? -INFINITY : -lse2 / c, delta);
   if constexpr (RB == 32) {  // the wavefronts' sums meet in the first one
     float* x = reinterpret_cast<float*>(tiles) + lane;
     if (wave > 0) {
@@ -940,7 +965,8 @@ __global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64)
       using First = std::integral_constant<short, 1>;
       using Last = std::integral_constant<short, 0>;
       const float* st = &stats[buf][0][at_t + 4 * half];
-      f32x16_t p;  // starts at -lse / scale: nothing is left to subtract
+      // bf16: the sum starts at -lse / scale, so that nothing is left to subtract; fp32 does not, since a sum near lse / scale rounds coarser
+      f32x16_t p;
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         const float4 v = *reinterpret_cast<const float4*>(st + 2 * i);
@@ -956,7 +982,11 @@ __global__ __launch_bounds__(2 * RB * P, sizeof(T) == 4 || (RB == 32 && D != 64)
           [&](int n) {
             if (n < KL) kl[n] = k_lds[n][threadIdx.x];
           },
-          p);
+          sizeof(T) == 2 ? p : zero16());
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] += st[row_of(i, 0)];
+      }
       const auto exponentials = [&](int n) { part_of_16<D>(n, [&](int i) { p[i] = __builtin_amdgcn_exp2f(p[i] * c); }); };
       f32x16_t dp = zero16();
       if constexpr (VL == 0) {

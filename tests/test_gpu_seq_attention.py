@@ -106,9 +106,13 @@ def check(torch, t, backward=True):
                 dp = torch.mm(do, v.t())
                 delta = (p * dp).sum(1, keepdim=True)
                 ds = p * (dp - delta) * scale
-                # delta comes from the stored out; both it and dp are sums of d products
-                ed = torch.mm(do.abs(), v.abs().t()) * (d + 4) * F32 + ((eo + (d + 4) * F32 * o.abs()) * do.abs()).sum(1, keepdim=True)
                 el = es + 8 * F32 + 8 * F32 * lse.masked_fill(none, 0).abs()[:, None]  # of p = exp(s - lse)
+                # dp and delta are sums of d products; delta comes from the stored out, in bf16 only where a row sees more than 128 keys
+                ed = torch.mm(do.abs(), v.abs().t()) * (d + 4) * F32
+                stored = ((eo + (d + 4) * F32 * o.abs()) * do.abs()).sum(1, keepdim=True)
+                if t["q"].dtype == torch.bfloat16 and (l <= 128 or 0 < t["window"] <= 128):
+                    stored = (el + (l + 8) * F32) * (stored + (p * (dp - delta)).abs().sum(1, keepdim=True)) + (d + 4) * F32 * (o.abs() * do.abs()).sum(1, keepdim=True)
+                ed = ed + stored
                 eds = (u + el) * ds.abs() + scale * p * ed * (1 + u)
                 near(t["dq"][s0:s0 + m, h], torch.mm(ds, k), torch.mm(eds + l * F32 * ds.abs(), k.abs()) + u * torch.mm(ds, k).abs(), "dq")
                 sums[0] += torch.mm(ds.t(), q)
@@ -137,6 +141,8 @@ SHAPES = [  # q_lens, k_lens, query heads, key heads, head_dim
     ([40, 200], [7, 130], 6, 2, 64),        # more queries than keys: with a causal mask the first ones see nothing
     ([17, 4], [400, 260], 12, 3, 128),      # a piece of a prompt behind earlier keys
     ([257], [257], 5, 5, 64),
+    ([2, 3, 1, 5], [2, 3, 1, 5], 2, 2, 128),  # gradients that are differences of few products
+    ([40] * 150, [40] * 150, 2, 2, 64),      # short ones in blocks of 128 rows
 ]
 MASKS = [(0, 0), (1, 0), (1, 1), (1, 50)]
 
@@ -197,6 +203,10 @@ def test_one_visible_key_has_no_gradient_and_runs_repeat(env):
     assert (t["dq"][:71] == 0).all() and (t["dk"][:71] == 0).all()
     for h in range(4):
         assert torch.equal(t["out"][:71, h], t["v"][:71, h // 2])
+    for q_lens, window, d in (([70, 1], 1, 32), ([1, 1, 1], 0, 128)):
+        t = case_tensors(torch, B, q_lens, q_lens, 16, 2, d, "float32", 1, window, "packed")
+        run(B, t)
+        assert (t["dq"][:sum(q_lens)] == 0).all() and (t["dk"][:sum(q_lens)] == 0).all()
     t = case_tensors(torch, B, [500, 33], [500, 33], 4, 2, 128, "bfloat16", 1, 0, "packed")
     run(B, t)
     first = [t[n].clone() for n in ("out", "lse", "dq", "dk", "dv")]
