@@ -8,6 +8,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <thread>
@@ -1514,6 +1515,13 @@ static mrem_status attention_sequences(const char* who, SeqAttn* a, const int32_
   a->q_start = q_start; a->k_start = k_start; a->q_len = q_len; a->k_len = k_len;
   return MREM_OK;
 }
+// outputs are written while inputs are still read: the mistakes that start at one address are refused
+static mrem_status attention_apart(const char* who, std::initializer_list<const void*> out, std::initializer_list<const void*> in) {
+  for (auto o = out.begin(); o != out.end(); ++o)
+    if (*o && (std::find(in.begin(), in.end(), *o) != in.end() || std::find(out.begin(), o, *o) != o))
+      return fail(nullptr, MREM_EINVAL, std::string(who) + ": an output is an input or another output");
+  return MREM_OK;
+}
 extern "C" size_t mrem_attention_workspace_bytes(const mrem_attention_config* cfg, int32_t backward) {
   SeqAttn a;
   if (attention_shape("mrem_attention_workspace_bytes", cfg, &a) != MREM_OK) return 0;
@@ -1536,6 +1544,7 @@ extern "C" mrem_status mrem_attention_forward(const mrem_attention_config* cfg, 
     REQUIRE_PTR(k, who);
     REQUIRE_PTR(v, who);
   }
+  if (const mrem_status st = attention_apart(who, {out, lse}, {q, a.k_rows ? k : nullptr, a.k_rows ? v : nullptr})) return st;
   a.q = q; a.k = k; a.v = v; a.out = out; a.lse = lse;
   seq_attn_fwd(a, workspace, (hipStream_t)hip_stream);
   return finish(nullptr, who);
@@ -1563,6 +1572,8 @@ extern "C" mrem_status mrem_attention_backward(const mrem_attention_config* cfg,
     REQUIRE_PTR(dk, who);
     REQUIRE_PTR(dv, who);
   }
+  if (const mrem_status st = attention_apart(who, {a.q_rows ? dq : nullptr, a.k_rows ? dk : nullptr, a.k_rows ? dv : nullptr},
+                                             {q, k, v, out, lse, d_out})) return st;
   a.q = q; a.k = k; a.v = v; a.out = const_cast<void*>(out); a.lse = const_cast<float*>(lse);
   a.dout = d_out; a.dq = dq; a.dk = dk; a.dv = dv;
   seq_attn_bwd(a, workspace, (hipStream_t)hip_stream);

@@ -91,6 +91,17 @@ def test_attention_refusals(B):
     assert B._lib.mrem_attention_forward(None, *[FAKE] * 10, 0, None) == B.MREM_EINVAL
 
 
+def test_attention_refuses_outputs_that_are_inputs(B):
+    cfg, tensors = attention_cfg(B), [ctypes.c_void_p(0x10000 * (i + 1)) for i in range(9)]
+    q, k, v, out, lse, do, dq, dk, dv = tensors
+    for o, l in ((q, lse), (k, lse), (v, lse), (out, q), (out, out)):
+        assert B._lib.mrem_attention_forward(ctypes.byref(cfg), q, k, v, FAKE, FAKE, None, None, o, l, FAKE, 1 << 40, None) == B.MREM_EINVAL
+        assert "output" in B.mrem_last_error()
+    for a, b, c in [(x, dk, dv) for x in tensors[:6]] + [(dq, x, dv) for x in tensors[:7]] + [(dq, dk, x) for x in tensors[:8]]:
+        assert B._lib.mrem_attention_backward(ctypes.byref(cfg), q, k, v, out, lse, do, FAKE, FAKE, None, None, a, b, c, FAKE, 1 << 40, None) == B.MREM_EINVAL
+        assert "output" in B.mrem_last_error()
+
+
 def test_distill_refusals(B):
     good = dict(x=FAKE, dtype=0, rows=4, vocab=100, ld=100, top=FAKE, index=FAKE, k=8, tlse=None, temp=1.0, w=None, scale=1.0, lr=FAKE, lo=FAKE, g=None, ldg=100)
     odd = ctypes.c_void_p(0x1001)
