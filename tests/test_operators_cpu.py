@@ -117,24 +117,25 @@ def test_distill_refusals(B):
 
 def test_binding_refuses_tensors_that_do_not_fit(B):
     import torch
-    q, k = torch.zeros(8, 4, 64), torch.zeros(8, 2, 64)
+    zeros = lambda *n, dtype=torch.float32: torch.zeros(*n, dtype=dtype)  # noqa: E731
+    q, k = zeros(8, 4, 64), zeros(8, 2, 64)
     for bad in (dict(q=q[:, :, ::2]), dict(q=q.transpose(0, 1)), dict(q=q.double()), dict(k=k.bfloat16()), dict(k=k[:7]), dict(q=q.reshape(8, 256)), dict(q=q[:7])):
         t = {"q": q, "k": k, "v": k, "out": q, **bad}
         with pytest.raises(ValueError):
             B.attention_config(t["q"], t["k"], t["v"], t["out"], 2)
     cfg = B.attention_config(q, k, k, q, 2, causal=1)
     assert (cfg.q_rows, cfg.q_heads, cfg.kv_heads, cfg.head_dim, cfg.ld_q, cfg.ld_k) == (8, 4, 2, 64, 256, 128)
-    lse, starts = torch.zeros(4, 8), torch.zeros(3, dtype=torch.int32)
-    for bad in (dict(q=q[:7]), dict(lse=lse.t().contiguous()), dict(q_start=starts[:2]), dict(q_start=starts.long()), dict(q=torch.zeros(8, 8, 64)[:, :4]), {}):  # the last: not on a GPU
+    lse, starts = zeros(4, 8), zeros(3, dtype=torch.int32)
+    for bad in (dict(q=q[:7]), dict(lse=lse.t().contiguous()), dict(q_start=starts[:2]), dict(q_start=starts.long()), dict(q=zeros(8, 8, 64)[:, :4]), {}):  # the last: not on a GPU
         t = {"q": q, "q_start": starts, "lse": lse, **bad}
         with pytest.raises(ValueError):
             B.mrem_attention_forward(cfg, t["q"], k, k, t["q_start"], starts, None, None, q, t["lse"], None)
-    x, z, i = torch.zeros(4, 100), torch.zeros(4, 8), torch.zeros(4, 8, dtype=torch.int32)
+    x, z, i = zeros(4, 100), zeros(4, 8), zeros(4, 8, dtype=torch.int32)
     for bad in (dict(x=x.t()), dict(x=x.half()), dict(z=z[:3]), dict(i=i.long()), dict(g=x.bfloat16()), dict(g=x[:, :99]), {}):
         t = {"x": x, "z": z, "i": i, "g": None, **bad}
         with pytest.raises(ValueError):
-            B.mrem_distill_loss(t["x"], t["z"], t["i"], None, 1.0, None, 1.0, torch.zeros(4), None, t["g"])
+            B.mrem_distill_loss(t["x"], t["z"], t["i"], None, 1.0, None, 1.0, zeros(4), None, t["g"])
     with pytest.raises(ValueError):
-        B.mrem_rotary_forward(q, q[:7], 64, 0, 1.0, torch.zeros(32, dtype=torch.float64))
+        B.mrem_rotary_forward(q, q[:7], 64, 0, 1.0, zeros(32, dtype=torch.float64))
     with pytest.raises(ValueError):
-        B.mrem_rotary_forward(q, q, 64, 0, 1.0, torch.zeros(32))
+        B.mrem_rotary_forward(q, q, 64, 0, 1.0, zeros(32))
