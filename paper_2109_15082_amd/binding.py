@@ -1,7 +1,8 @@
 """ctypes binding of libmrem.so: argument marshalling only.
 
 Every function has the name and the argument order of its C declaration in
-include/mrem.h.  Tensors are torch tensors on the GPU (torch is used for device
+include/mrem.h; those of the operators outside the module step take sizes and
+strides from the tensors and keep the order of what is left.  Tensors are torch tensors on the GPU (torch is used for device
 memory and streams only); every step of the method runs in the HIP kernels of
 the library.  Importing this module fails if the library has not been built
 (python -m paper_2109_15082_amd.build): there is no fallback path.

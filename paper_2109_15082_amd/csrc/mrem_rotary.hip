@@ -1,6 +1,6 @@
 // Rotary positions: the first values of every head are turned in pairs by position * frequency.
 //
-// Each value is read and written once, so memory bounds it.  A block takes one to four rows: its threads first form the sine and
+// Each value is read and written once, so memory bounds it (8192 rows, 40 heads of 128 in bf16: 37 us, 4.5 TB/s; a copy reaches 5.2).  A block takes one to four rows: its threads first form the sine and
 // cosine of every pair of those rows, which all heads share, and then walk the rows' heads in pieces of 16 bytes (two of them
 // where a pair's halves lie apart).  A position times a frequency needs more than 32 bits as soon as the angle has passed some
 // thousand turns, so the angle is formed in 64 bits in units of turns, and what is left of a whole turn is rounded to 32.
