@@ -183,3 +183,19 @@ def test_no_rows_and_replays(env):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(loss, want[0]) and torch.equal(rows, want[1]) and torch.equal(grad, want[2])
+
+
+@pytest.mark.parametrize("vocab", [1003, 140001])
+def test_rows_far_apart(env, vocab):
+    """offsets that pass 2^31 elements, of rows that a block holds and of rows that it reads twice"""
+    torch, B = env
+    rows, ld = 600, 1 << 22
+    s = inputs(torch, rows, vocab, 9, "bfloat16", 1)
+    want = run(torch, B, s)
+    near, far = s["x"], torch.full((rows, ld), math.nan, device="cuda", dtype=torch.bfloat16)
+    s["x"] = far[:, 5:5 + vocab]
+    s["x"].copy_(near)
+    loss_rows, loss = torch.empty(rows, device="cuda"), torch.empty(1, device="cuda")
+    B.mrem_distill_loss(s["x"], s["z"], s["at"], s["lse"], 1.0, s["w"], 1.0, loss_rows, loss, s["x"])
+    assert torch.equal(loss, want[0]) and torch.equal(loss_rows, want[1]) and torch.equal(s["x"], want[2])
+    assert far[:, :5].isnan().all() and far[:, 5 + vocab:].isnan().all()

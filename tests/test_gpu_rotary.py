@@ -90,3 +90,21 @@ def test_more_rows_than_a_launch_has_blocks(env):
     pos = torch.arange(n, device="cuda", dtype=torch.int32)
     B.mrem_rotary_forward(x, y, 2, 1, 1.0, freq.cuda(), pos)
     check(torch, y, *turned(torch, x, pos, freq, 2, 1, 1.0, 1), 1.0)
+
+
+def test_rows_far_apart(env):
+    """offsets that pass 2^31 elements, in pieces and value by value"""
+    torch, B = env
+    rows, ld = 1100, 1 << 21
+    whole, freq = torch.full((rows, ld), 7.0, device="cuda", dtype=torch.bfloat16), B.mrem_rotary_frequencies(64).cuda()
+    x = torch.randn(rows, 2, 64, device="cuda").bfloat16()
+    for odd in (0, 3):
+        near = torch.empty(rows, 128 + odd, device="cuda", dtype=torch.bfloat16).as_strided((rows, 2, 64), (128 + odd, 64, 1))
+        far = whole.as_strided((rows, 2, 64), (ld - odd, 64, 1))
+        near.copy_(x)
+        far.copy_(x)
+        for y in (near, far):
+            B.mrem_rotary_forward(y, y, 64, 0, 1.0, freq)
+        assert torch.equal(far, near)
+        far.fill_(7.0)
+    assert (whole == 7).all()

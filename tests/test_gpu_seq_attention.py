@@ -331,3 +331,25 @@ def test_captured_and_replayed_on_another_stream(env):
         t["q"].mul_(0.5)                      # other inputs, eagerly, between the replays
         run(B, t)
         want = [t[n].clone() for n in names]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_rows_as_far_apart_as_allowed(env, dtype):
+    """queries, keys and values side by side in rows of 2^21 elements, and their gradients: offsets pass 2^31 elements and 2^32 bytes"""
+    torch, B = env
+    hq, hk, d, ld = 4, 2, 64, 1 << 21
+    for q_lens, k_lens in (([700, 400], [600, 500]), ([1, 1], [900, 300])):
+        t = case_tensors(torch, B, q_lens, k_lens, hq, hk, d, dtype, 1, 0, "packed", spare=0)
+        rows, at = max(sum(q_lens), sum(k_lens)), {"q": 0, "k": hq + 1, "v": hq + hk + 2}
+        heads = {"q": hq, "k": hk, "v": hk}
+        for names, fill in ((("q", "k", "v"), math.nan), (("dq", "dk", "dv"), 3.0), (("out",), 3.0), (("dout",), math.nan)):
+            whole = torch.full((rows, ld), fill, device="cuda", dtype=t["q"].dtype)
+            for name in names:
+                n = {"out": "q", "dout": "q"}.get(name, name[-1])
+                new = whole.as_strided((t[name].shape[0], heads[n], d), (ld, d, 1), at[n] * d)
+                new.copy_(t[name])
+                t[name] = new
+        t["cfg"] = B.attention_config(t["q"], t["k"], t["v"], t["out"], len(q_lens), 1, 0)
+        assert t["cfg"].ld_q == t["cfg"].ld_v == t["cfg"].ld_out == ld
+        run(B, t)
+        check(torch, t)
