@@ -586,9 +586,10 @@ __global__ __launch_bounds__(kThreads, (kForwardWaves<T, D, RB>)) void seq_fwd_k
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[e][r] *= f;
       }
-      const float mc = m == -INFINITY ? 0.f : m * c;
+      // fp32: the difference first, so that a single key's exponential is one and its output the value to the bit
+      const float m0 = m == -INFINITY ? 0.f : m, mc = m0 * c;
       const auto exponential = [&](int t, int r) {
-        p[t][r] = __builtin_amdgcn_exp2f(fmaf(p[t][r], c, -mc));
+        p[t][r] = __builtin_amdgcn_exp2f(sizeof(T) == 4 ? (p[t][r] - m0) * c : fmaf(p[t][r], c, -mc));
         l += p[t][r];
       };
 #pragma unroll
@@ -774,9 +775,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : D == 128 || RB == 32
   };
   // delta of a stored output is off by the output's rounding, which is what most of a row's gradient is made of where it sees few keys (a
   // row's gradient is a difference of its few products).  There a first pass takes the sum of the score gradients, which is zero but for
-  // that error, back from delta: rows of up to 128 keys.  With more the error is below the rounding of the gradient itself.  (Two tokens
-  // of 128 wide heads in bf16: gradients 5.6e-3 off without it, 1.7e-3 with it; a row that sees one key has none, to the bit, in either type.)
-  const bool twice = (a.window ? min(a.window, j_hi) : j_hi) <= 128;
+  // that error, back from delta: rows of up to 128 keys in bf16.  With more the error is below the rounding of the gradient itself, and fp32
+  // rounds an output no more than the products' sums.  (Two tokens of 128 wide heads in bf16: gradients 5.6e-3 off without it, 1.7e-3 with
+  // it.  In fp32 it would cost 15.8 instead of 12.4 us for four sentences of up to 77 tokens, 12 heads of 64.)
+  const bool twice = sizeof(T) == 2 && (a.window ? min(a.window, j_hi) : j_hi) <= 128;
   // gradients of the scores of keys [j, j + 32), rows `at` of the tile
   const auto score_gradients = [&](int at, int j) {
     f32x16_t p = rows_times<T, D>(Ks, at, lane, [&](int kk) { return qf[kk]; });
